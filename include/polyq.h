@@ -432,6 +432,127 @@ polyq_status polyq_bit_scaling(const float* w, int32_t n, int32_t k, const doubl
                                const double* saliency, const int32_t* bits, const float* grid,
                                int32_t ngrid, float* scale, float* alpha);
 
+/*
+ * ---- Microscaled 4-bit floating point (MXFP4) ------------------------------
+ * A matrix [rows][k] whose rows are cut into blocks of 32 consecutive values
+ * (the last one may be shorter).  A value is a 4-bit code: bit 3 the sign, bits
+ * 0..2 the magnitude {0, 0.5, 1, 1.5, 2, 3, 4, 6}; a block's values share the
+ * scale 2^(byte - 127), byte in 0..254; byte 255 makes the whole block NaN.
+ *
+ * Packed matrix (device, 256-byte aligned, polyq_mx_bytes bytes): tiles of 16
+ * rows, tile t at t * tile_bytes; a tile holds its records of 512 channels in
+ * order, every record but the last 4352 bytes:
+ *     [scales: 256 B][chunk 0: 1024 B] .. [chunk 3: 1024 B]
+ * (the last one only the chunks of 128 channels that k reaches into).  Byte
+ * 16 l .. 16 l + 15 of chunk c hold the 32 codes, low half first, of row l % 16
+ * and the channels 128 c + 32 (l / 16) .. + 31 of the record, l = 0 .. 63; byte
+ * 4 l + c of the scales is that block's scale byte: what a 64-lane 16x16x128
+ * matrix instruction takes from lane l.  Rows and channels behind the last are
+ * code 0 with scale byte 127.
+ *
+ * The conventions at the head of this file hold: nothing is allocated, calls only
+ * enqueue work, argument errors are found before any launch (POLYQ_ERR_ARG: a null
+ * or misaligned pointer, a type or activation that is none of those below, m < 1;
+ * POLYQ_ERR_SHAPE: rows, n or k outside 1 .. POLYQ_MAX_N, POLYQ_MAX_K;
+ * POLYQ_ERR_CAPACITY: the workspace is too small or the launch too large).
+ * Pointers to fp32, fp16 and bf16 arrays need the alignment of one element;
+ * arrays on 16 bytes with rows of whole 16-byte vectors are read faster.
+ */
+#define POLYQ_MX_BLOCK 32 /* values that share a scale */
+
+/* Element types (int32_t arguments); POLYQ_MX_PACKED: a packed matrix in place of activations. */
+enum { POLYQ_MX_F32 = 0, POLYQ_MX_F16 = 1, POLYQ_MX_BF16 = 2, POLYQ_MX_PACKED = 3 };
+
+/* Activations of the gated block: g / (1 + exp(-g)); g Phi(g) with the normal distribution
+ * function; and the latter's tanh form, g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2. */
+enum { POLYQ_ACT_SILU = 0, POLYQ_ACT_GELU = 1, POLYQ_ACT_GELU_TANH = 2 };
+
+/* Bytes of a packed matrix; 0 if rows or k is out of range. */
+size_t polyq_mx_bytes(int32_t rows, int32_t k);
+
+/*
+ * polyq_mx_quantize -- x [rows][k] of `type` into a packed matrix: a block's scale
+ * is 2^(floor(log2 max|v|) - 2), at least 2^-127; v / scale goes to the nearest
+ * magnitude, ties to the even code, what lies above 6 to 6.  A block that holds an
+ * infinity or a NaN becomes NaN.  `packed` is fully overwritten.
+ */
+polyq_status polyq_mx_quantize(const void* x, int32_t type, int32_t rows, int32_t k, void* packed,
+                               void* stream);
+
+/* polyq_mx_dequantize -- the values of a packed matrix as [rows][k] of `type`, rounded once. */
+polyq_status polyq_mx_dequantize(const void* packed, int32_t rows, int32_t k, void* out,
+                                 int32_t type, void* stream);
+
+/*
+ * polyq_mx_pack, polyq_mx_unpack -- a checkpoint's codes uint8 [rows][ceil(k / 2)]
+ * (channel 2 i in the low half of byte i) and scale bytes uint8 [rows][ceil(k / 32)]
+ * into a packed matrix and back.  For an odd k the upper half of a row's last byte is
+ * ignored by the one and written as 0 by the other.
+ */
+polyq_status polyq_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t rows, int32_t k,
+                           void* packed, void* stream);
+polyq_status polyq_mx_unpack(const void* packed, int32_t rows, int32_t k, uint8_t* codes,
+                             uint8_t* scales, void* stream);
+
+/*
+ * polyq_mx_linear -- y = q(x) W^T for any m >= 1 tokens:
+ *   x  [m][k] of x_type, quantized as by polyq_mx_quantize, or a packed matrix [m][k]
+ *      (x_type POLYQ_MX_PACKED), which several products can share;
+ *   w  packed [n][k];  y  [m][n] of y_type, fully overwritten.
+ *   workspace: polyq_mx_workspace_bytes(m, k, x_type) bytes of device scratch, 256-byte
+ *   aligned (the packed x; NULL where that is 0); its contents on entry are ignored.
+ *   Calls that share one must be ordered.
+ * Products of two 4-bit values are exact and summed in fp32; y is rounded once.  Sums
+ * are added in a fixed order: the same call gives the same bits.
+ */
+size_t polyq_mx_workspace_bytes(int32_t m, int32_t k, int32_t x_type);
+polyq_status polyq_mx_linear(const void* x, int32_t x_type, int32_t m, const void* w, int32_t n,
+                             int32_t k, void* y, int32_t y_type, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * polyq_mx_gated -- the gated feed-forward block's first half in one launch:
+ *   h = act(g) u,  g = q(x) G^T,  u = q(x) U^T   (g, u and act in fp32, h rounded once)
+ * gate and up packed [n][k], h [m][n] of h_type; x and workspace as for polyq_mx_linear.
+ */
+polyq_status polyq_mx_gated(const void* x, int32_t x_type, int32_t m, const void* gate,
+                            const void* up, int32_t n, int32_t k, int32_t act, void* h,
+                            int32_t h_type, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * polyq_mx_linear_backward -- gradients of polyq_mx_linear, the rounding passed by
+ * as if it were the identity:
+ *   dx = dy W  [m][k],   dw = dy^T q(x)  [n][k],   both of grad_type, either NULL to skip
+ *   (not both; x may be NULL where dw is).  dy [m][n] of dy_type.
+ * The products run on the bf16 matrix cores, summed in fp32: W and q(x) are exact in
+ * bf16, dy enters as one bf16 value where grad_type is bf16, as the sum of two for
+ * fp16 (to 2^-17) and of three for fp32 (exactly).
+ *   workspace: polyq_mx_linear_backward_workspace_bytes(m, n, k, x_type, grad_type, dx,
+ *   dw) bytes (dx, dw: whether that gradient is asked for), 256-byte aligned.
+ */
+size_t polyq_mx_linear_backward_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t x_type,
+                                                int32_t grad_type, int32_t dx, int32_t dw);
+polyq_status polyq_mx_linear_backward(const void* dy, int32_t dy_type, const void* x,
+                                      int32_t x_type, int32_t m, const void* w, int32_t n,
+                                      int32_t k, void* dx, void* dw, int32_t grad_type,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * polyq_mx_gated_backward -- gradients of polyq_mx_gated from dh [m][n]; g and u are
+ * computed again from x, gate and up:
+ *   dg = dh u act'(g),  du = dh act(g)   in fp32, then as dy above,
+ *   dx = dg G + du U,  dgate = dg^T q(x),  dup = du^T q(x),
+ * of grad_type; dx, or dgate and dup together, may be NULL to skip them.  workspace as
+ * above (polyq_mx_gated_backward_workspace_bytes).
+ */
+size_t polyq_mx_gated_backward_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t x_type,
+                                               int32_t grad_type, int32_t dx, int32_t dw);
+polyq_status polyq_mx_gated_backward(const void* dh, int32_t dh_type, const void* x,
+                                     int32_t x_type, int32_t m, const void* gate, const void* up,
+                                     int32_t n, int32_t k, int32_t act, void* dx, void* dgate,
+                                     void* dup, int32_t grad_type, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
 /* Static description of a status code (never NULL). */
 const char* polyq_status_str(polyq_status status);
 

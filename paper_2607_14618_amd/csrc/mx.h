@@ -1,0 +1,169 @@
+// Shared definitions of the microscaled 4-bit (MXFP4) operators: the packed layout
+// (include/polyq.h, polyq_mx_bytes), the operand fragments it is made of, element
+// types and the gated block's activations.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace polyq {
+namespace mx {
+
+constexpr int kBlock = POLYQ_MX_BLOCK;  // values that share a scale
+constexpr int kRows = 16;               // rows of a packed tile: the rows of one matrix instruction
+constexpr int kChunk = 128;             // values of a row that one matrix instruction takes
+constexpr int kChunkBytes = kRows * kChunk / 2;
+constexpr int kRec = 4 * kChunk;        // values of a row that one 4-byte word of scales covers
+constexpr int kScaleBytes = 256;        // scales of a record: a word per lane, its byte c of chunk c
+constexpr int kRecBytes = kScaleBytes + 4 * kChunkBytes;
+constexpr int kNanScale = 255;
+
+typedef int i4v __attribute__((ext_vector_type(4)));
+typedef int i8v __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+__host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
+__host__ __device__ inline int chunks_of(int k) { return div_up(k, kChunk); }
+__host__ __device__ inline int records_of(int k) { return div_up(k, kRec); }
+__host__ __device__ inline int tiles_of(int rows) { return div_up(rows, kRows); }
+__host__ __device__ inline int64_t tile_bytes(int k) {
+  return static_cast<int64_t>(records_of(k)) * kScaleBytes + static_cast<int64_t>(chunks_of(k)) * kChunkBytes;
+}
+// Offset of a chunk's codes and of its record's scales inside a tile.
+__host__ __device__ inline int64_t chunk_offset(int c) {
+  return static_cast<int64_t>(c >> 2) * kRecBytes + kScaleBytes + (c & 3) * kChunkBytes;
+}
+__host__ __device__ inline int64_t scale_offset(int c) { return static_cast<int64_t>(c >> 2) * kRecBytes; }
+
+// 2^(byte - 127) as a float; 255 as NaN.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  const uint32_t bits = byte == 0 ? 0x00400000u : byte == kNanScale ? 0x7fc00000u : byte << 23;
+  return __builtin_bit_cast(float, bits);
+}
+
+// 16 rows x 128 channels of A (rows of D) by 16 rows x 128 channels of B (columns of D), every
+// 32-channel block of a row with its scale in byte `SEL` of that lane's word.  Products
+// of two 4-bit values are exact and the sums are kept in fp32.
+template <int SEL_A, int SEL_B>
+__device__ __forceinline__ f4 mfma_mx(i4v a, i4v b, f4 c, int sa, int sb) {
+  const i8v x = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, y = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, SEL_A, sa, SEL_B, sb);
+}
+
+// ------------------------------------------------------------------ element types
+struct F32 { typedef float type; };
+struct F16 { typedef _Float16 type; };
+struct BF16 { typedef __bf16 type; };
+
+inline bool float_type(int t) { return t == POLYQ_MX_F32 || t == POLYQ_MX_F16 || t == POLYQ_MX_BF16; }
+inline int type_bytes(int t) { return t == POLYQ_MX_F32 ? 4 : 2; }
+
+template <class T>
+__device__ __forceinline__ float load1(const T* p) { return static_cast<float>(*p); }
+
+// Four consecutive elements; vec: p is aligned to all four.
+template <class T>
+__device__ __forceinline__ f4 load4(const T* p, bool vec, int valid) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  f4 v = {0.f, 0.f, 0.f, 0.f};
+  if (vec && valid >= 4) {
+    const t4 r = *reinterpret_cast<const t4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(r[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < valid) v[i] = static_cast<float>(p[i]);
+  }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ void store4(T* p, f4 v, bool vec, int valid) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  if (vec && valid >= 4) {
+    t4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = static_cast<T>(v[i]);
+    *reinterpret_cast<t4*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < valid) p[i] = static_cast<T>(v[i]);
+  }
+}
+// The same with the type known at run time.
+__device__ __forceinline__ f4 load4(const void* base, int type, int64_t at, bool vec, int valid) {
+  if (type == POLYQ_MX_F32) return load4(static_cast<const float*>(base) + at, vec, valid);
+  if (type == POLYQ_MX_F16) return load4(static_cast<const _Float16*>(base) + at, vec, valid);
+  return load4(static_cast<const __bf16*>(base) + at, vec, valid);
+}
+__device__ __forceinline__ void store4(void* base, int type, int64_t at, f4 v, bool vec, int valid) {
+  if (type == POLYQ_MX_F32) store4(static_cast<float*>(base) + at, v, vec, valid);
+  else if (type == POLYQ_MX_F16) store4(static_cast<_Float16*>(base) + at, v, vec, valid);
+  else store4(static_cast<__bf16*>(base) + at, v, vec, valid);
+}
+
+// The next bf16 terms of fp32 values, and what they leave of them (nothing of one that is not finite in bf16).
+__device__ __forceinline__ bf16x4 next_terms(f4* v) {
+  bf16x4 t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    t[i] = static_cast<__bf16>((*v)[i]);
+    const float f = static_cast<float>(t[i]);
+    (*v)[i] = __builtin_isfinite(f) ? (*v)[i] - f : 0.f;
+  }
+  return t;
+}
+
+// ------------------------------------------------------------------ activations
+// act(g) and, if asked for, act'(g), in fp32:
+//   silu       g s,  s = 1 / (1 + exp(-g));        s (1 + g (1 - s))
+//   gelu       g P,  P = erfc(-g / sqrt 2) / 2;    P + g exp(-g^2 / 2) / sqrt(2 pi)
+//   gelu_tanh  g s,  s = 1 / (1 + exp(-2 z)) = (1 + tanh z) / 2,
+//              z = sqrt(2 / pi) (g + 0.044715 g^3);  s + g s (1 - s) 2 z'
+__device__ __forceinline__ float activation(int act, float g, float* slope) {
+  if (act == POLYQ_ACT_GELU) {
+    const float p = 0.5f * erfcf(g * -0.70710678118654752f);
+    if (slope) *slope = p + g * (0.39894228040143268f * expf(-0.5f * g * g));
+    return g * p;
+  }
+  if (act == POLYQ_ACT_GELU_TANH) {
+    const float a = 0.79788456080286536f, b = 0.044715f, g2 = g * g;
+    const float s = 1.f / (1.f + expf(-2.f * a * g * (1.f + b * g2)));
+    // s (1 - s) is 0 where z' overflows the product
+    if (slope) *slope = s + (s == 0.f || s == 1.f ? 0.f : g * s * (1.f - s) * 2.f * a * (1.f + 3.f * b * g2));
+    return g * s;
+  }
+  const float s = 1.f / (1.f + expf(-g));
+  if (slope) *slope = s * (1.f + g * (1.f - s));
+  return g * s;
+}
+inline bool valid_act(int act) { return act == POLYQ_ACT_SILU || act == POLYQ_ACT_GELU || act == POLYQ_ACT_GELU_TANH; }
+
+// ------------------------------------------------------------------ host side
+inline bool valid_shape(int32_t rows, int32_t k) {
+  return rows >= 1 && rows <= POLYQ_MAX_N && k >= 1 && k <= POLYQ_MAX_K;
+}
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// x [rows][k] into the packed layout (arguments checked by the caller).
+polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, void* packed, hipStream_t st);
+
+// dg and du of the gated block as bf16 planes [terms][m_pad][2][n_pad] (zero behind m and
+// n), whose sum over the terms is the fp32 value: to 2^-9, 2^-17 and 2^-25 of it with one,
+// two and three.  x is packed.
+polyq_status launch_gated_grad(const void* gate, const void* up, const void* x, const void* dh, int dh_type, int32_t m,
+                               int32_t n, int32_t k, int act, void* planes, int terms, int32_t m_pad, int32_t n_pad,
+                               hipStream_t st);
+
+}  // namespace mx
+}  // namespace polyq

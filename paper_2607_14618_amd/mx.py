@@ -1,0 +1,259 @@
+"""Microscaled 4-bit floating point (MXFP4) on one GPU: quantization, the linear layer,
+the gated feed-forward block and their gradients (marshalling around the C ABI)."""
+from __future__ import annotations
+
+import contextlib
+from typing import Optional, Tuple, Union
+
+import torch
+
+from . import _lib
+from ._lib import _aligned_empty, _check, _need_cuda, _ptr, _stream, lib
+
+BLOCK = 32
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+PACKED = 3
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+class MXMatrix:
+    """A packed matrix [rows][k] in microscaled 4-bit floating point (polyq.h), as
+    ``mx_quantize`` and ``mx_pack`` make it."""
+
+    __slots__ = ("rows", "k", "packed")
+
+    def __init__(self, rows: int, k: int, packed: torch.Tensor):
+        self.rows, self.k, self.packed = rows, k, packed
+
+    @property
+    def shape(self) -> Tuple[int, int]:
+        return self.rows, self.k
+
+    @property
+    def device(self) -> torch.device:
+        return self.packed.device
+
+    def __repr__(self):
+        return f"MXMatrix(rows={self.rows}, k={self.k}, device={self.device})"
+
+
+def _on(dev: torch.device):
+    """Launches go to the tensors' device, whatever the current one is."""
+    if dev.index is None or dev.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(dev)
+
+
+def _type(t: torch.dtype, what: str) -> int:
+    if t not in TYPES:
+        raise ValueError(f"{what} must be fp32, fp16 or bf16, got {t}")
+    return TYPES[t]
+
+
+def _two(x: torch.Tensor, what: str) -> torch.Tensor:
+    if x.dim() not in (1, 2):
+        raise ValueError(f"{what} must be [rows][columns] or one row")
+    return x if x.dim() == 2 else x.reshape(1, -1)
+
+
+def _empty_matrix(rows: int, k: int, dev: torch.device) -> MXMatrix:
+    nbytes = int(lib().polyq_mx_bytes(rows, k))
+    if nbytes == 0:
+        raise ValueError(f"a matrix of {rows} rows x {k} channels cannot be packed")
+    return MXMatrix(rows, k, _aligned_empty(nbytes, dev))
+
+
+def mx_quantize(x: torch.Tensor) -> MXMatrix:
+    """x [rows][k] (fp32, fp16 or bf16; one row as [k]) in microscaled 4 bits."""
+    t = _type(x.dtype, "x")
+    x2 = _two(x, "x")
+    dev = _need_cuda(x2)
+    out = _empty_matrix(x2.shape[0], x2.shape[1], dev)
+    with _on(dev):
+        _check(lib().polyq_mx_quantize(_ptr(x2), t, out.rows, out.k, _ptr(out.packed), _stream(dev)),
+               "polyq_mx_quantize")
+    return out
+
+
+def mx_dequantize(q: MXMatrix, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """The values of a packed matrix, [rows][k]."""
+    t = _type(dtype, "dtype")
+    dev = _need_cuda(q.packed)
+    out = torch.empty((q.rows, q.k), dtype=dtype, device=dev)
+    with _on(dev):
+        _check(lib().polyq_mx_dequantize(_ptr(q.packed), q.rows, q.k, _ptr(out), t, _stream(dev)),
+               "polyq_mx_dequantize")
+    return out
+
+
+def mx_pack(codes: torch.Tensor, scales: torch.Tensor, k: int) -> MXMatrix:
+    """A checkpoint's codes uint8 [rows][ceil(k / 2)] (even channels in the low halves) and
+    scale bytes uint8 [rows][ceil(k / 32)] as a packed matrix."""
+    dev = _need_cuda(codes, scales)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2:
+        raise ValueError("codes and scales must be uint8 [rows][..]")
+    if tuple(codes.shape) != (codes.shape[0], (k + 1) // 2):
+        raise ValueError(f"codes shape {tuple(codes.shape)} is not [rows][{(k + 1) // 2}]")
+    if tuple(scales.shape) != (codes.shape[0], -(-k // BLOCK)):
+        raise ValueError(f"scales shape {tuple(scales.shape)} is not [{codes.shape[0]}][{-(-k // BLOCK)}]")
+    out = _empty_matrix(codes.shape[0], int(k), dev)
+    with _on(dev):
+        _check(lib().polyq_mx_pack(_ptr(codes), _ptr(scales), out.rows, out.k, _ptr(out.packed), _stream(dev)),
+               "polyq_mx_pack")
+    return out
+
+
+def mx_unpack(q: MXMatrix) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(codes, scales) of a packed matrix, as ``mx_pack`` takes them."""
+    dev = _need_cuda(q.packed)
+    codes = torch.empty((q.rows, (q.k + 1) // 2), dtype=torch.uint8, device=dev)
+    scales = torch.empty((q.rows, -(-q.k // BLOCK)), dtype=torch.uint8, device=dev)
+    with _on(dev):
+        _check(lib().polyq_mx_unpack(_ptr(q.packed), q.rows, q.k, _ptr(codes), _ptr(scales), _stream(dev)),
+               "polyq_mx_unpack")
+    return codes, scales
+
+
+Activations = Union[torch.Tensor, MXMatrix]
+
+
+def _input(x: Activations, *ws: MXMatrix):
+    """(x's pointer, its type, tokens, the default output type) with the weights' shapes checked."""
+    for w in ws:
+        if not isinstance(w, MXMatrix):
+            raise ValueError("weights must be packed (mx_quantize or mx_pack)")
+        if w.shape != ws[0].shape:
+            raise ValueError(f"gate {ws[0].shape} and up {w.shape} must have the same shape")
+    if isinstance(x, MXMatrix):
+        t, m, k, out, held = PACKED, x.rows, x.k, torch.bfloat16, x.packed
+    else:
+        t, held = _type(x.dtype, "x"), _two(x, "x")
+        m, k, out = held.shape[0], held.shape[1], x.dtype
+    if k != ws[0].k:
+        raise ValueError(f"x has {k} channels, the weights have {ws[0].k}")
+    return held, t, m, out
+
+
+def _output(y: Optional[torch.Tensor], shape, dtype: torch.dtype, dev: torch.device, what: str) -> torch.Tensor:
+    if y is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if tuple(y.shape) != tuple(shape) or y.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)}, got {y.dtype} {tuple(y.shape)}")
+    return y
+
+
+def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev: torch.device):
+    """(pointer, bytes, tensor): the caller's, or memory of this call alone (torch hands it out in the
+    stream's order, so that neither two streams nor two captured graphs share it)."""
+    if workspace is None and nbytes:
+        workspace = _aligned_empty(nbytes, dev)
+    if workspace is None:
+        return None, 0, None
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _product(name: str, x: Activations, ws, act: Optional[str], dtype, y, workspace):
+    held, t, m, out = _input(x, *ws)
+    dev = _need_cuda(held, y, workspace, *(w.packed for w in ws))
+    dtype = y.dtype if dtype is None and y is not None else out if dtype is None else dtype
+    ot = _type(dtype, "the output")
+    y = _output(y, (m, ws[0].rows), dtype, dev, "the output")
+    L = lib()
+    need = 0 if t == PACKED else int(L.polyq_mx_workspace_bytes(m, ws[0].k, t))
+    ptr, nbytes, _keep = _scratch(workspace, need, dev)
+    n, k = ws[0].shape
+    with _on(dev):
+        if act is None:
+            st = L.polyq_mx_linear(_ptr(held), t, m, _ptr(ws[0].packed), n, k, _ptr(y), ot, ptr, nbytes, _stream(dev))
+        else:
+            st = L.polyq_mx_gated(_ptr(held), t, m, _ptr(ws[0].packed), _ptr(ws[1].packed), n, k, ACTIVATIONS[act],
+                                  _ptr(y), ot, ptr, nbytes, _stream(dev))
+    _check(st, name)
+    return y
+
+
+def mx_linear(x: Activations, w: MXMatrix, dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [m][n] = q(x) W^T, q(x) the microscaled 4-bit form of x.  x is [m][k] (fp32,
+    fp16 or bf16; one row as [k]) or a packed matrix, which several products can share;
+    y has x's type (bf16 for a packed x) unless ``dtype`` or ``y`` says otherwise."""
+    return _product("polyq_mx_linear", x, (w,), None, dtype, y, workspace)
+
+
+def mx_gated(x: Activations, gate: MXMatrix, up: MXMatrix, act: str = "silu", dtype: Optional[torch.dtype] = None,
+             y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """h [m][n] = act(q(x) gate^T) * (q(x) up^T) in one launch; act: "silu", "gelu" or
+    "gelu_tanh".  x, dtype and y as for ``mx_linear``."""
+    _act(act)
+    return _product("polyq_mx_gated", x, (gate, up), act, dtype, y, workspace)
+
+
+def _act(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {tuple(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def _incoming(d: torch.Tensor, m: int, n: int, what: str):
+    d2 = _two(d, what)
+    if tuple(d2.shape) != (m, n):
+        raise ValueError(f"{what} must be [{m}][{n}], got {tuple(d2.shape)}")
+    return d2, _type(d.dtype, what)
+
+
+def mx_linear_backward(dy: torch.Tensor, x: Optional[Activations], w: MXMatrix, dtype: Optional[torch.dtype] = None,
+                       need_dx: bool = True, need_dw: bool = True, workspace: Optional[torch.Tensor] = None
+                       ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dx [m][k], dw [n][k]) of ``mx_linear``, None for one that is not asked for: dx = dy W,
+    dw = dy^T q(x), the rounding to 4 bits passed by as the identity.  The gradients
+    have ``dtype`` (dy's type by default).  x may be None where dw is not asked for."""
+    if not isinstance(w, MXMatrix):
+        raise ValueError("weights must be packed (mx_quantize or mx_pack)")
+    if not (need_dx or need_dw):
+        raise ValueError("neither dx nor dw is asked for")
+    if need_dw:
+        if x is None:
+            raise ValueError("dw needs x")
+        held, t, m, _ = _input(x, w)
+    else:
+        held, t, m = None, PACKED, _two(dy, "dy").shape[0]
+    d, dt = _incoming(dy, m, w.rows, "dy")
+    dev = _need_cuda(d, held, w.packed, workspace)
+    dtype = dy.dtype if dtype is None else dtype
+    gt = _type(dtype, "dtype")
+    dx = torch.empty((m, w.k), dtype=dtype, device=dev) if need_dx else None
+    dw = torch.empty((w.rows, w.k), dtype=dtype, device=dev) if need_dw else None
+    L = lib()
+    need = int(L.polyq_mx_linear_backward_workspace_bytes(m, w.rows, w.k, t, gt, need_dx, need_dw))
+    ptr, nbytes, _keep = _scratch(workspace, need, dev)
+    with _on(dev):
+        _check(L.polyq_mx_linear_backward(_ptr(d), dt, _ptr(held), t, m, _ptr(w.packed), w.rows, w.k, _ptr(dx), _ptr(dw),
+                                          gt, ptr, nbytes, _stream(dev)), "polyq_mx_linear_backward")
+    return dx, dw
+
+
+def mx_gated_backward(dh: torch.Tensor, x: Activations, gate: MXMatrix, up: MXMatrix, act: str = "silu",
+                      dtype: Optional[torch.dtype] = None, need_dx: bool = True, need_dw: bool = True,
+                      workspace: Optional[torch.Tensor] = None):
+    """(dx [m][k], dgate [n][k], dup [n][k]) of ``mx_gated``, None for those not asked for;
+    g and u are computed again, so that the forward pass keeps nothing but x.  The
+    gradients have ``dtype`` (dh's type by default)."""
+    a = _act(act)
+    if not (need_dx or need_dw):
+        raise ValueError("neither dx nor the weights' gradients are asked for")
+    held, t, m, _ = _input(x, gate, up)
+    n, k = gate.shape
+    d, dt = _incoming(dh, m, n, "dh")
+    dev = _need_cuda(d, held, gate.packed, up.packed, workspace)
+    dtype = dh.dtype if dtype is None else dtype
+    gt = _type(dtype, "dtype")
+    dx = torch.empty((m, k), dtype=dtype, device=dev) if need_dx else None
+    dg, du = (torch.empty((n, k), dtype=dtype, device=dev) if need_dw else None for _ in range(2))
+    L = lib()
+    need = int(L.polyq_mx_gated_backward_workspace_bytes(m, n, k, t, gt, need_dx, need_dw))
+    ptr, nbytes, _keep = _scratch(workspace, need, dev)
+    with _on(dev):
+        _check(L.polyq_mx_gated_backward(_ptr(d), dt, _ptr(held), t, m, _ptr(gate.packed), _ptr(up.packed), n, k, a,
+                                         _ptr(dx), _ptr(dg), _ptr(du), gt, ptr, nbytes, _stream(dev)),
+               "polyq_mx_gated_backward")
+    return dx, dg, du
