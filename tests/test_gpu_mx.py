@@ -1,0 +1,461 @@
+"""Microscaled 4-bit operators on the GPU against a plain implementation in 64 bits.
+
+Tolerances.  Products of 4-bit values and powers of two are exact; what rounds is
+  * the fp32 sums: at most one unit in the last place (2^-23) of the running sum per
+    128-channel step, so 2^-23 (steps + 8) times the sum of magnitudes;
+  * the result's type, half a step relative to it: fp32 2^-24, fp16 2^-11, bf16 2^-8 (and the
+    smallest subnormal's half for fp16);
+  * in the gated block act(g): its argument carries g's error times the slope (at most 1.13 in
+    magnitude), exp, erfc and the divisions a few units of 2^-24;
+  * in the gradients the incoming factor as one bf16 value (2^-8) for bf16, two (2^-16) for
+    fp16, three (2^-24) for fp32.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_14618_amd as pq
+from gpu_util import dev
+
+pytestmark = pytest.mark.gpu
+
+F = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+HALF = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TERM = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -16, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+def quantized(x):
+    """(values, codes, scale bytes) of x [rows][k] by the definition, in 64 bits on the CPU."""
+    v = x.detach().cpu().double().numpy()
+    rows, k = v.shape
+    nb = -(-k // 32)
+    p = np.zeros((rows, nb * 32))
+    p[:, :k] = v
+    p = p.reshape(rows, nb, 32)
+    top = np.abs(p).max(2)
+    bad = ~np.isfinite(p).all(2)
+    e = np.where((top > 0) & ~bad, np.frexp(np.where(bad, 1.0, top))[1] - 3, -127)
+    e = np.maximum(e, -127)
+    a = np.where(bad[:, :, None], 0.0, np.abs(np.where(np.isfinite(p), p, 0.0)) / np.exp2(e.astype(np.float64))[:, :, None])
+    mid = (GRID[1:] + GRID[:-1]) / 2
+    low, high = np.searchsorted(mid, a, "left"), np.searchsorted(mid, a, "right")
+    code = np.where(low % 2 == 0, low, high)
+    val = GRID[code] * np.exp2(e.astype(np.float64))[:, :, None] * np.where(np.signbit(p), -1.0, 1.0)
+    val[bad] = np.nan
+    code = code + 8 * np.signbit(p)
+    code[bad] = 0
+    byte = np.where(bad, 255, e + 127)
+    return (torch.from_numpy(val.reshape(rows, -1)[:, :k].copy()), code.reshape(rows, -1)[:, :k].astype(np.uint8),
+            byte.astype(np.uint8))
+
+
+def activations(m, k, t, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((m, k), generator=g)
+    x[:, :: max(1, k // 5)] *= 20
+    return x.to(F[t])
+
+
+def weights(n, k, seed):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn((n, k), generator=g) * 0.05
+    return w
+
+
+def same(a, b):
+    a, b = a.detach().cpu().double(), b.double()
+    return bool(torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b)))
+
+
+def within(got, want, tol, what):
+    """|got - want| <= tol elementwise; `got` is compared as it is, `want` and `tol` are 64-bit CPU tensors."""
+    g = got.detach().cpu().double()
+    assert torch.isfinite(g).all(), what
+    off = (g - want).abs()
+    at = int((off - tol).argmax())
+    assert bool((off <= tol).all()), f"{what}: off {off.flatten()[at]:.3e}, allowed {tol.flatten()[at]:.3e}"
+
+
+def sum_tol(mag, k):
+    return 2.0 ** -23 * (-(-k // 128) + 8) * mag
+
+
+def out_tol(want, t):
+    return HALF[t] * want.abs() + TINY[t]
+
+
+# ------------------------------------------------------------------ quantization
+@pytest.mark.parametrize("t", list(F))
+@pytest.mark.parametrize("rows,k", [(1, 1), (1, 32), (3, 31), (16, 128), (17, 129), (5, 511), (33, 512), (2, 513),
+                                    (40, 1000), (1, 5120), (19, 2976), (100, 1357)])
+def test_quantize_is_the_definition(rows, k, t):
+    x = activations(rows, k, t, seed=rows * 7 + k)
+    if k > 64:
+        x[0, :64] = 0                  # a block of zeros
+        x[-1, 32:64] = 1e-7            # a small one (subnormal in fp16)
+    val, code, byte = quantized(x)
+    q = pq.mx_quantize(x.to(dev()))
+    assert same(pq.mx_dequantize(q), val)
+    codes, scales = pq.mx_unpack(q)
+    want = np.zeros((rows, (k + 1) // 2 * 2), dtype=np.uint8)
+    want[:, :k] = code
+    assert np.array_equal(codes.cpu().numpy(), want[:, 0::2] + 16 * want[:, 1::2])
+    assert np.array_equal(scales.cpu().numpy(), byte)
+    for name, typ in F.items():
+        assert same(pq.mx_dequantize(q, dtype=typ), val.to(torch.float32).to(typ).double())
+    again = pq.mx_pack(codes, scales, k)
+    assert torch.equal(again.packed, q.packed), "pack(unpack(q)) is q, its padding among it"
+
+
+def test_quantize_rounds_ties_to_even_and_saturates():
+    mags = [0.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 7.99]
+    rows = []
+    for e in (-126, -100, -3, 0, 5, 100, 125):
+        for nudge in (-1, 0, 1):
+            row = torch.zeros(32, dtype=torch.float64)
+            row[0] = 4.0                                   # the block's largest: scale 2^0 before 2^e
+            for i, v in enumerate(mags[:7]):
+                f = np.float32(v)
+                f = np.nextafter(f, np.float32(nudge * 1e9)) if nudge and v else f
+                row[1 + 2 * i], row[2 + 2 * i] = float(f), -float(f)
+            rows.append(row * 2.0 ** e)
+            rows.append(torch.tensor(mags + [-m for m in mags] + [0.0] * 10, dtype=torch.float64) * 2.0 ** min(e, 124))
+    x = torch.stack(rows).float()
+    val, code, byte = quantized(x)
+    q = pq.mx_quantize(x.to(dev()))
+    assert same(pq.mx_dequantize(q), val)
+
+
+def test_quantize_extreme_blocks():
+    big, tiny = torch.finfo(torch.float32).max, 2.0 ** -149
+    x = torch.zeros((8, 96))
+    x[0, :32], x[1, :32] = big, tiny
+    x[2, 0], x[2, 33] = float("inf"), 1.0
+    x[3, 40] = float("nan")
+    x[4, 95] = -float("inf")
+    x[5, :] = 2.0 ** -126
+    x[6, 3] = -0.0
+    val, code, byte = quantized(x)
+    q = pq.mx_quantize(x.to(dev()))
+    assert same(pq.mx_dequantize(q), val)
+    assert np.array_equal(pq.mx_unpack(q)[1].cpu().numpy(), byte)
+    assert torch.isnan(pq.mx_dequantize(q, dtype=torch.bfloat16)[2, :32]).all()
+
+
+def test_quantize_reads_unaligned_rows():
+    x = activations(9, 512, "bf16", 3).to(dev())
+    flat = torch.empty(9 * 512 + 1, dtype=torch.bfloat16, device=dev())
+    flat[1:] = x.flatten()
+    view = flat[1:].view(9, 512)           # 2 bytes behind a 16-byte boundary
+    assert view.data_ptr() % 16 == 2
+    assert torch.equal(pq.mx_quantize(view).packed, pq.mx_quantize(x).packed)
+
+
+# ------------------------------------------------------------------ linear, gated
+SHAPES = [(1, 1, 1), (1, 16, 128), (2, 17, 129), (1, 100, 5120), (16, 130, 640), (5, 64, 2976), (17, 33, 515),
+          (33, 1357, 513), (77, 200, 2976), (64, 256, 1024), (130, 300, 384), (257, 129, 640), (16, 5120, 160)]
+
+
+@pytest.mark.parametrize("t", list(F))
+@pytest.mark.parametrize("m,n,k", SHAPES)
+def test_linear(m, n, k, t):
+    x, w = activations(m, k, t, m + n), weights(n, k, n + k)
+    xv, wv = quantized(x)[0], quantized(w)[0]
+    want, mag = xv @ wv.T, xv.abs() @ wv.abs().T
+    wq = pq.mx_quantize(w.to(dev()))
+    y = pq.mx_linear(x.to(dev()), wq)
+    assert y.dtype == F[t] and tuple(y.shape) == (m, n)
+    tol = sum_tol(mag, k) + out_tol(want, F[t])
+    within(y, want, tol, "linear")
+    assert torch.equal(y, pq.mx_linear(x.to(dev()), wq)), "the same call gives the same bits"
+    packed = pq.mx_quantize(x.to(dev()))
+    assert torch.equal(y, pq.mx_linear(packed, wq, dtype=F[t])), "a packed x gives the same result"
+    y32 = pq.mx_linear(packed, wq, dtype=torch.float32)
+    within(y32, want, sum_tol(mag, k) + out_tol(want, torch.float32), "linear fp32")
+
+
+def act64(act, g):
+    if act == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s))
+    if act == "gelu":
+        p = 0.5 * torch.erfc(-g / 2 ** 0.5)
+        return g * p, p + g * torch.exp(-g * g / 2) / (2 * np.pi) ** 0.5
+    z, dz = (2 / np.pi) ** 0.5 * (g + 0.044715 * g ** 3), (2 / np.pi) ** 0.5 * (1 + 3 * 0.044715 * g * g)
+    th = torch.tanh(z)
+    return 0.5 * g * (1 + th), 0.5 * (1 + th) + 0.5 * g * (1 - th * th) * dz
+
+
+def gated64(x, gate, up, act):
+    """xv, gv, uv (quantized values), g, u, their fp32 error bounds, act(g), act'(g)."""
+    xv, gv, uv = quantized(x)[0], quantized(gate)[0], quantized(up)[0]
+    g, u = xv @ gv.T, xv @ uv.T
+    k = x.shape[1]
+    return xv, gv, uv, g, u, sum_tol(xv.abs() @ gv.abs().T, k), sum_tol(xv.abs() @ uv.abs().T, k), *act64(act, g)
+
+
+# an act of magnitude |g| p: p from exp/erfc/divide, each within 4 units of 2^-24 relative, an argument of
+# exp as large as |2 z| or g^2 / 2 scaling that by its own rounding (2^-24 relative of the argument)
+def act_tol(g, a):
+    arg = torch.clamp(1 + g.abs() + g * g + 0.1 * g.abs() ** 3, max=120.0)
+    return 2.0 ** -24 * (16 + 4 * arg) * a.abs() + 1e-30
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("t", list(F))
+@pytest.mark.parametrize("m,n,k", [(1, 16, 128), (1, 1, 3), (3, 100, 5120), (16, 130, 640), (33, 77, 515),
+                                   (130, 300, 384), (257, 129, 640)])
+def test_gated(m, n, k, t, act):
+    x, gate, up = activations(m, k, t, m + n), weights(n, k, 1), weights(n, k, 2)
+    _, _, _, g, u, eg, eu, a, _ = gated64(x, gate, up, act)
+    want = a * u
+    h = pq.mx_gated(x.to(dev()), pq.mx_quantize(gate.to(dev())), pq.mx_quantize(up.to(dev())), act=act)
+    assert h.dtype == F[t] and tuple(h.shape) == (m, n)
+    ea = 1.2 * eg + act_tol(g, a)
+    tol = ea * u.abs() + (a.abs() + ea) * eu + 2.0 ** -23 * want.abs()
+    within(h, want, tol * (1 + HALF[F[t]]) + out_tol(want, F[t]), f"gated {act}")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_gated_far_arguments(act):
+    """g of +-2^6 .. 2^30 with u = 1: act(g) is g or 0, its slope 1 or 0, without NaN."""
+    k, n = 32, 61
+    x = torch.zeros((1, k))
+    x[0, 0] = 4.0                       # exact in 4 bits
+    gate, up = torch.zeros((n, k)), torch.zeros((n, k))
+    for i in range(n):
+        gate[i, 0] = (-1) ** i * 2.0 ** (4 + i // 2)
+        up[i, 0] = 0.25
+    args = [pq.mx_quantize(v.to(dev())) for v in (gate, up)]
+    g = 4.0 * gate[:, 0].double()
+    h = pq.mx_gated(x.to(dev()), *args, act=act)
+    a, da = act64(act, g)
+    assert torch.isfinite(h).all()
+    assert bool(((h.cpu().double()[0] - a).abs() <= 2.0 ** -20 * g.abs() * (g > 0) + 1e-20).all())
+    dx, dg, du = pq.mx_gated_backward(torch.ones((1, n), device=dev()), x.to(dev()), *args, act=act)
+    assert torch.isfinite(dx).all() and torch.isfinite(dg).all() and torch.isfinite(du).all()
+    assert bool(((dg.cpu().double()[:, 0] - 4.0 * da).abs() <= 1e-5 * 4).all())
+
+
+def test_linear_propagates_nan_and_only_there():
+    x, w = activations(20, 256, "fp32", 5), weights(40, 256, 6)
+    x[3, 100] = float("nan")
+    w[7, 10] = float("inf")
+    y = pq.mx_linear(x.to(dev()), pq.mx_quantize(w.to(dev()))).cpu()
+    nan = torch.isnan(y)
+    want = torch.zeros_like(nan)
+    want[3, :], want[:, 7] = True, True
+    assert torch.equal(nan, want)
+
+
+# ------------------------------------------------------------------ gradients
+BACK = [(1, 1, 1), (1, 16, 128), (7, 33, 129), (64, 64, 256), (65, 130, 384), (77, 1357, 515), (200, 257, 640),
+        (16, 640, 1000)]
+
+
+@pytest.mark.parametrize("t", list(F))
+@pytest.mark.parametrize("m,n,k", BACK)
+def test_linear_backward(m, n, k, t):
+    typ = F[t]
+    x, w = activations(m, k, t, m + 1), weights(n, k, n + 1)
+    dy = torch.randn((m, n), generator=torch.Generator().manual_seed(9)).to(typ)
+    xv, wv, d = quantized(x)[0], quantized(w)[0], dy.double()
+    wq = pq.mx_quantize(w.to(dev()))
+    dx, dw = pq.mx_linear_backward(dy.to(dev()), x.to(dev()), wq)
+    assert dx.dtype == dw.dtype == typ
+    terms = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 3}[typ]
+    for got, want, mag, length in ((dx, d @ wv, d.abs() @ wv.abs(), n), (dw, d.T @ xv, d.abs().T @ xv.abs(), m)):
+        # an input of the gradients' own type enters exactly
+        tol = 2.0 ** -23 * (terms * (length // 32 + 2) + 40) * mag + out_tol(want, typ)
+        within(got, want, tol, "linear_backward")
+    only, none = pq.mx_linear_backward(dy.to(dev()), None, wq, need_dw=False)
+    assert none is None and torch.equal(only, dx)
+    none, only = pq.mx_linear_backward(dy.to(dev()), pq.mx_quantize(x.to(dev())), wq, need_dx=False)
+    assert none is None and torch.equal(only, dw)
+
+
+@pytest.mark.parametrize("dt,gt", [("fp32", "bf16"), ("fp32", "fp16"), ("bf16", "fp32"), ("fp16", "bf16")])
+def test_linear_backward_mixed_types(dt, gt):
+    m, n, k = 50, 70, 300
+    x, w = activations(m, k, "bf16", 1), weights(n, k, 2)
+    dy = torch.randn((m, n), generator=torch.Generator().manual_seed(9)).to(F[dt])
+    xv, wv, d = quantized(x)[0], quantized(w)[0], dy.double()
+    dx, dw = pq.mx_linear_backward(dy.to(dev()), x.to(dev()), pq.mx_quantize(w.to(dev())), dtype=F[gt])
+    for got, want, mag in ((dx, d @ wv, d.abs() @ wv.abs()), (dw, d.T @ xv, d.abs().T @ xv.abs())):
+        assert got.dtype == F[gt]
+        within(got, want, (TERM[F[gt]] + 2.0 ** -23 * 60) * mag * (1 + HALF[F[gt]]) + out_tol(want, F[gt]), "mixed types")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("t", list(F))
+@pytest.mark.parametrize("m,n,k", [(1, 1, 3), (1, 16, 128), (7, 33, 129), (65, 130, 384), (77, 357, 515), (200, 257, 640)])
+def test_gated_backward(m, n, k, t, act):
+    typ = F[t]
+    x, gate, up = activations(m, k, t, m + 1), weights(n, k, 1), weights(n, k, 2)
+    dh = torch.randn((m, n), generator=torch.Generator().manual_seed(9)).to(typ)
+    xv, gv, uv, g, u, eg, eu, a, da = gated64(x, gate, up, act)
+    d = dh.double()
+    dg, du = d * u * da, d * a
+    # errors of dg, du: g and u in fp32 (act'' is at most 1.2 in magnitude), act and act', the products, the terms
+    curve = 1.2 * eg + act_tol(g, da) + act_tol(g, a)
+    e_dg = d.abs() * (curve * (u.abs() + eu) + eu * da.abs()) + (TERM[typ] + 2.0 ** -22) * dg.abs()
+    e_du = d.abs() * (1.2 * eg + act_tol(g, a)) + (TERM[typ] + 2.0 ** -22) * du.abs()
+    got = pq.mx_gated_backward(dh.to(dev()), x.to(dev()), pq.mx_quantize(gate.to(dev())), pq.mx_quantize(up.to(dev())),
+                               act=act)
+    terms = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 3}[typ]
+    for what, out, want, mag, err, length in (
+            ("dx", got[0], dg @ gv + du @ uv, dg.abs() @ gv.abs() + du.abs() @ uv.abs(), e_dg @ gv.abs() + e_du @ uv.abs(), 2 * n),
+            ("dgate", got[1], dg.T @ xv, dg.abs().T @ xv.abs(), e_dg.T @ xv.abs(), m),
+            ("dup", got[2], du.T @ xv, du.abs().T @ xv.abs(), e_du.T @ xv.abs(), m)):
+        assert out.dtype == typ
+        tol = err + 2.0 ** -23 * (terms * (length // 32 + 2) + 40) * (mag + err)
+        within(out, want, tol * (1 + HALF[typ]) + out_tol(want, typ), f"{what} {act}")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_gated_gradient_against_differences(act):
+    """x and the weights on values that 4 bits hold, where the operator is the smooth function of them: the
+    kernel's gradients against central differences of that function in 64 bits.  A difference of step h
+    is off by h^2 / 6 times the third derivative and 2^-52 / h of the value: with h = 1e-5 far below
+    the 2^-20 allowed, which counts the fp32 errors of a sum of 64 terms."""
+    m, n, k = 4, 8, 64
+    g = torch.Generator().manual_seed(4)
+    pick = lambda *s: torch.from_numpy(GRID)[torch.randint(0, 8, s, generator=g)] * (1 - 2 * torch.randint(0, 2, s, generator=g))
+    x, gate, up = pick(m, k) / 4, pick(n, k) / 16, pick(n, k) / 16
+    x[:, ::32], gate[:, ::32], up[:, ::32] = 1.5, 0.375, 0.375   # every block's largest is at 6 of its scale
+    dh = torch.randn((m, n), generator=g)
+
+    def f(x, gate, up):
+        a = act64(act, x @ gate.T)[0]
+        return float((a * (x @ up.T) * dh.double()).sum())
+
+    for v in (x, gate, up):
+        assert same(pq.mx_dequantize(pq.mx_quantize(v.float().to(dev()))), v)
+    got = pq.mx_gated_backward(dh.to(dev()), x.float().to(dev()), pq.mx_quantize(gate.float().to(dev())),
+                               pq.mx_quantize(up.float().to(dev())), act=act)
+    h = 1e-5
+    for which, out in enumerate(got):
+        out = out.cpu().double()
+        for i, j in ((0, 0), (1, 33), (2, 17), (3, 63)):
+            args = [[v.clone() for v in (x, gate, up)] for _ in range(2)]
+            args[0][which][i, j] += h
+            args[1][which][i, j] -= h
+            diff = (f(*args[0]) - f(*args[1])) / (2 * h)
+            assert abs(float(out[i, j]) - diff) <= 2.0 ** -20 * 64 * max(1.0, abs(diff)), (which, i, j)
+
+
+# ------------------------------------------------------------------ together, streams, graphs
+def test_feed_forward_block_and_its_gradients_together():
+    """gate, up, activation and down as a model calls them, forward and backward, with h and dh between the
+    operators taken from the GPU so that each one's error is its own."""
+    m, k, n = 50, 384, 300
+    x = activations(m, k, "bf16", 1)
+    gate, up, down = weights(n, k, 1), weights(n, k, 2), weights(k, n, 3)
+    gq, uq, dq = (pq.mx_quantize(w.to(dev())) for w in (gate, up, down))
+    shared = pq.mx_quantize(x.to(dev()))
+    h = pq.mx_gated(shared, gq, uq)
+    assert torch.equal(h, pq.mx_gated(x.to(dev()), gq, uq))
+    y = pq.mx_linear(h, dq)
+    hv, wv = quantized(h)[0], quantized(down)[0]
+    want = hv @ wv.T
+    within(y, want, sum_tol(hv.abs() @ wv.abs().T, n) + out_tol(want, torch.bfloat16), "down")
+    dy = torch.randn((m, k), generator=torch.Generator().manual_seed(3)).bfloat16().to(dev())
+    dh, ddown = pq.mx_linear_backward(dy, h, dq)
+    d = dy.cpu().double()
+    within(dh, d @ wv, 2.0 ** -17 * (d.abs() @ wv.abs()) + out_tol(d @ wv, torch.bfloat16), "dh")
+    within(ddown, d.T @ hv, 2.0 ** -17 * (d.abs().T @ hv.abs()) + out_tol(d.T @ hv, torch.bfloat16), "ddown")
+    a = pq.mx_gated_backward(dh, shared, gq, uq)
+    b = pq.mx_gated_backward(dh, x.to(dev()), gq, uq)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_two_streams_at_once():
+    x = [activations(16, 1024, "fp16", s).to(dev()) for s in range(2)]
+    w = [pq.mx_quantize(weights(2000, 1024, s).to(dev())) for s in range(2)]
+    want = [pq.mx_linear(x[i], w[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(pq.mx_linear(x[i], w[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(v, want[i]) for v in got[i])
+
+
+@pytest.mark.parametrize("m", [1, 16, 100])
+def test_graph_replays_match_eager(m):
+    """Two graphs captured one after the other and replayed in turn, eager calls between the replays."""
+    k, n = 640, 300
+    gq, uq = pq.mx_quantize(weights(n, k, 1).to(dev())), pq.mx_quantize(weights(n, k, 2).to(dev()))
+    dh = torch.randn((m, n), generator=torch.Generator().manual_seed(3)).bfloat16().to(dev())
+    xs = [activations(m, k, "bf16", s).to(dev()) for s in range(2)]
+
+    def step(x):
+        h = pq.mx_gated(x, gq, uq, act="gelu")
+        y = pq.mx_linear(x, gq, dtype=torch.float32)
+        return [h, y, *pq.mx_gated_backward(dh, x, gq, uq, act="gelu"), *pq.mx_linear_backward(dh, x, gq)]
+
+    want = [step(x) for x in xs]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in xs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(x))
+        graphs.append(g)
+    for _ in range(3):
+        for i in (1, 0, 1):
+            for o in outs[i]:
+                o.fill_(float("nan"))
+            graphs[i].replay()
+            eager = step(xs[1 - i])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
+            assert all(torch.equal(a, b) for a, b in zip(eager, want[1 - i]))
+
+
+def test_nothing_is_written_outside_the_outputs():
+    """Outputs inside larger buffers: the bytes around them keep their sentinel."""
+    m, n, k = 19, 37, 200
+    x, w = activations(m, k, "fp32", 1).to(dev()), pq.mx_quantize(weights(n, k, 2).to(dev()))
+    buf = torch.full((m * n + 64,), 7.0, device=dev())
+    y = buf[32:32 + m * n].view(m, n)
+    pq.mx_linear(x, w, y=y)
+    assert bool((buf[:32] == 7).all()) and bool((buf[32 + m * n:] == 7).all())
+    assert torch.equal(y, pq.mx_linear(x, w))
+    raw = torch.full((int(pq.lib().polyq_mx_bytes(m, k)) + 512,), 0xAB, dtype=torch.uint8, device=dev())
+    off = (-raw.data_ptr()) % 256
+    nbytes = int(pq.lib().polyq_mx_bytes(m, k))
+    assert pq.lib().polyq_mx_quantize(x.data_ptr(), 0, m, k, raw.data_ptr() + off, None) == 0
+    torch.cuda.synchronize()
+    assert bool((raw[:off] == 0xAB).all()) and bool((raw[off + nbytes:] == 0xAB).all())
+    assert torch.equal(raw[off:off + nbytes], pq.mx_quantize(x).packed)
+
+
+@pytest.mark.slow
+def test_offsets_past_32_bits():
+    """A packed weight of more than 2^31 bytes, and more than 2^32 weights: its last rows are right."""
+    n, k = 270000, 32768
+    codes = torch.zeros((n, k // 2), dtype=torch.uint8, device=dev())
+    scales = torch.full((n, k // 32), 127, dtype=torch.uint8, device=dev())
+    g = torch.Generator(device=dev()).manual_seed(1)
+    rows = torch.tensor([0, 1, 131071, 131072, n - 17, n - 1], device=dev())
+    codes[rows] = torch.randint(0, 256, (len(rows), k // 2), generator=g, device=dev()).to(torch.uint8)
+    w = pq.mx_pack(codes, scales, k)
+    assert w.packed.numel() > 2 ** 32
+    x = activations(3, k, "bf16", 2)
+    few = pq.mx_pack(codes[rows].contiguous(), scales[rows].contiguous(), k)
+    want = pq.mx_linear(x.to(dev()), few, dtype=torch.float32)
+    wide = pq.mx_linear(torch.cat([x] * 7).to(dev()), w, dtype=torch.float32)   # 21 tokens
+    y = pq.mx_linear(x.to(dev()), w, dtype=torch.float32)
+    assert torch.equal(y[:, rows], want) and torch.equal(wide[:3, rows], want)
+    rest = y.clone()
+    rest[:, rows] = 0
+    assert not bool(rest.any())
+    got, s = pq.mx_unpack(w)
+    assert torch.equal(got[rows], codes[rows]) and torch.equal(s[rows], scales[rows])
