@@ -21,20 +21,21 @@ struct Args {
   int32_t m, n, k;
   int32_t y_type, dh_type, act;
   int32_t y_vec, dh_vec;      // rows of y / dh take vector accesses of four elements
-  int32_t terms, m_pad, n_pad;  // kGatedGrad: planes bf16 [terms][m_pad][2][n_pad]
+  int32_t terms, m_pad, n_pad;  // kGatedGrad: planes [terms][2][m_pad][n_pad]
   int32_t token_blocks;
 };
 
-// Four consecutive outputs (rows n0 .. n0 + 3 of the weights) of one token.
-template <int MODE>
+// Four consecutive outputs (rows n0 .. n0 + 3 of the weights) of one token.  WHOLE: all of them and the token
+// are there, and rows take vector accesses.
+template <int MODE, class T, bool WHOLE>
 __device__ __forceinline__ void finish(const Args& a, int token, int n0, f4 v, f4 u) {
   if (MODE == kGatedGrad) {
     // du = dh act(g), dg = dh u act'(g) as sums of bf16 terms; zero in the padding
-    if (token >= a.m_pad || n0 >= a.n_pad) return;
+    if (!WHOLE && (token >= a.m_pad || n0 >= a.n_pad)) return;
     f4 dg = {0.f, 0.f, 0.f, 0.f}, du = {0.f, 0.f, 0.f, 0.f};
-    if (token < a.m && n0 < a.n) {
-      const int valid = a.n - n0;
-      const f4 d = load4(a.dh, a.dh_type, static_cast<int64_t>(token) * a.n + n0, a.dh_vec, valid);
+    if (WHOLE || (token < a.m && n0 < a.n)) {
+      const int valid = WHOLE ? 4 : a.n - n0;
+      const f4 d = load4(static_cast<const T*>(a.dh) + static_cast<int64_t>(token) * a.n + n0, WHOLE || a.dh_vec, valid);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i >= valid) break;
@@ -44,20 +45,19 @@ __device__ __forceinline__ void finish(const Args& a, int token, int n0, f4 v, f
         du[i] = d[i] * act;
       }
     }
-    __bf16* out = static_cast<__bf16*>(a.y) + static_cast<int64_t>(token) * 2 * a.n_pad + n0;
-    const int64_t plane = static_cast<int64_t>(a.m_pad) * 2 * a.n_pad;
+    const int64_t plane = static_cast<int64_t>(a.m_pad) * a.n_pad * 2;
+    uint8_t* out = static_cast<uint8_t*>(a.y) + plane_at(token, n0, a.n_pad);
     for (int t = 0; t < a.terms; ++t) {
-      const bf16x4 g4 = next_terms(&dg), u4 = next_terms(&du);
-      *reinterpret_cast<bf16x4*>(out + t * plane) = g4;
-      *reinterpret_cast<bf16x4*>(out + t * plane + a.n_pad) = u4;
+      *reinterpret_cast<bf16x4*>(out + 2 * t * plane) = next_terms(&dg);
+      *reinterpret_cast<bf16x4*>(out + (2 * t + 1) * plane) = next_terms(&du);
     }
   } else {
-    if (token >= a.m || n0 >= a.n) return;
+    if (!WHOLE && (token >= a.m || n0 >= a.n)) return;
     if (MODE == kGated) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = activation(a.act, v[i], nullptr) * u[i];
     }
-    store4(a.y, a.y_type, static_cast<int64_t>(token) * a.n + n0, v, a.y_vec, a.n - n0);
+    store4(static_cast<T*>(a.y) + static_cast<int64_t>(token) * a.n + n0, v, WHOLE || a.y_vec, WHOLE ? 4 : a.n - n0);
   }
 }
 
@@ -134,21 +134,25 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
 #pragma unroll
       for (int w = 1; w < W; ++w) v[h] += sums[w][(h * PT + i) * TM + j][l];
     }
-    finish<MODE>(a, (tok0 + j) * kRows + (l & 15), (tile0 + i) * kRows + (l >> 4) * 4, v[0], v[NM - 1]);
+    const int token = (tok0 + j) * kRows + (l & 15), n0 = (tile0 + i) * kRows + (l >> 4) * 4;
+    if (a.y_type == POLYQ_MX_BF16) finish<MODE, __bf16, false>(a, token, n0, v[0], v[NM - 1]);
+    else if (a.y_type == POLYQ_MX_F16) finish<MODE, _Float16, false>(a, token, n0, v[0], v[NM - 1]);
+    else finish<MODE, float, false>(a, token, n0, v[0], v[NM - 1]);
   }
 }
 
 // ---------------------------------------------------------------- many tokens
-// WN x WM waves, each TN row tiles (the gated modes: TN / 2 of each matrix) by TM token
-// tiles.  K is walked KC chunks at a time: the fragments of both operands go from
-// memory straight into one half of a ring in LDS while the other half is multiplied.
-template <int MODE, int WN, int WM, int TN, int TM, int KC>
-__global__ __launch_bounds__(64 * WN * WM) void mx_gemm_kernel(const Args a) {
-  constexpr int W = WN * WM, RT = WN * TN, CT = WM * TM, SLOTS = RT + CT;
+// WN x WM waves, each TN x 32 rows (the gated modes: TN / 2 x 32 of each matrix) by TM x 32
+// tokens.  K is walked a record (4 chunks) at a time.  The tokens' fragments go from
+// memory straight into one half of a ring in LDS while the other half is multiplied; the
+// weights' fragments are what their wave alone multiplies and go into its registers,
+// two chunks ahead.
+template <int MODE, int WN, int WM, int TN, int TM>
+__global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) {
+  constexpr int W = WN * WM, CT = WM * TM;
   constexpr int NM = MODE == kLinear ? 1 : 2, PT = TN / NM;
-  constexpr int STAGE = SLOTS * KC * kChunkBytes;
-  constexpr int LOADS = SLOTS * KC / W;
-  static_assert(SLOTS * KC % W == 0 && 4 % KC == 0, "tile");
+  constexpr int STAGE = CT * 8 * kChunkBytes, LOADS = CT * 8 / W;
+  static_assert(CT * 8 % W == 0, "tile");
   extern __shared__ uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wn = wave % WN, wm = wave / WN;
@@ -161,98 +165,152 @@ __global__ __launch_bounds__(64 * WN * WM) void mx_gemm_kernel(const Args a) {
   const int chunks = chunks_of(a.k), records = records_of(a.k);
   const int row_tiles = tiles_of(a.n), token_tiles = tiles_of(a.m);
   const int64_t tb = tile_bytes(a.k);
-  // Slot s of a stage: row tile s of the work-group (s = wn TN + i), then its token tiles.
-  auto slot_ptr = [&](int s) -> const uint8_t* {
-    if (s < RT) {
-      const int sw = s / TN, i = s % TN;
-      return a.w[i / PT] + min((rb * WN + sw) * PT + i % PT, row_tiles - 1) * tb;
-    }
-    return a.x + min(tbk * CT + s - RT, token_tiles - 1) * tb;
-  };
-  const uint8_t* src[LOADS];
+  // Of a pair of row tiles, lanes 16 .. 31 and 48 .. 63 take the second (the first again where there is none).
+  const int second = (lane >> 4) & 1, at16 = (lane >> 5) * 256 + (lane & 15) * 16, at4 = at16 >> 2;
+  // Buffers that begin at the work-group's first tiles; a lane's offsets of its tiles inside them.
+  const int row0 = min(rb * WN * PT * 2, row_tiles - 1), tok0 = min(tbk * CT * 2, token_tiles - 1);
+  const __amdgpu_buffer_rsrc_t wbuf0 = make_rsrc(a.w[0] + row0 * tb, (row_tiles - row0) * tb);
+  const __amdgpu_buffer_rsrc_t wbuf1 = make_rsrc(a.w[NM - 1] + row0 * tb, (row_tiles - row0) * tb);
+  const __amdgpu_buffer_rsrc_t xbuf = make_rsrc(a.x + tok0 * tb, (token_tiles - tok0) * tb);
+  const uint32_t tb32 = static_cast<uint32_t>(tb);
+  uint32_t wo[PT], xo[TM];
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) src[i] = slot_ptr((i * W + wave) / KC);
-  auto fetch = [&](int c, int half) {  // chunks c .. c + KC - 1 (the last one again past the end)
+  for (int i = 0; i < PT; ++i) wo[i] = (min(((rb * WN + wn) * PT + i) * 2 + second, row_tiles - 1) - row0) * tb32;
+#pragma unroll
+  for (int j = 0; j < TM; ++j) xo[j] = (min((tbk * CT + wm * TM + j) * 2 + second, token_tiles - 1) - tok0) * tb32;
+  auto chunk_at = [&](int c) { return static_cast<uint32_t>(chunk_offset(min(c, chunks - 1))); };  // the last again past the end
+  auto fetch = [&](int rec, int half) {  // the tokens' codes of a record
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int piece = i * W + wave;
-      const int64_t at = chunk_offset(min(c + piece % KC, chunks - 1));
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(src[i] + at + lane * 16),
-          (__attribute__((address_space(3))) void*)(lds + half * STAGE + piece * kChunkBytes), 16, 0, 0);
+      const uint32_t tile = (min(tbk * CT * 2 + piece / 4, token_tiles - 1) - tok0) * tb32;
+      load_to_lds(xbuf, lds + half * STAGE + piece * kChunkBytes, lane * 16, tile + chunk_at(rec * 4 + piece % 4));
     }
   };
-  const uint8_t* sa_ptr[TN];
-  const uint8_t* sb_ptr[TM];
-#pragma unroll
-  for (int i = 0; i < TN; ++i) sa_ptr[i] = slot_ptr(wn * TN + i) + lane * 4;
-#pragma unroll
-  for (int j = 0; j < TM; ++j) sb_ptr[j] = slot_ptr(RT + wm * TM + j) + lane * 4;
-  int sa[TN], sb[TM], na[TN], nb[TM];
+  // Scales of the record at hand and of the next one.
+  int sa[TN][2], sb[TM][2], na[TN][2], nb[TM][2];
   auto scales = [&](int rec) {
-    const int64_t at = static_cast<int64_t>(min(rec, records - 1)) * kRecBytes;
+    const uint32_t at = static_cast<uint32_t>(min(rec, records - 1)) * kRecBytes;
 #pragma unroll
-    for (int i = 0; i < TN; ++i) na[i] = *reinterpret_cast<const int*>(sa_ptr[i] + at);
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int j = 0; j < TM; ++j) nb[j] = *reinterpret_cast<const int*>(sb_ptr[j] + at);
+      for (int i = 0; i < TN; ++i)
+        na[i][h] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(i < PT ? wbuf0 : wbuf1, wo[i % PT] + at4 + h * 128, at, 0));
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+        nb[j][h] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(xbuf, xo[j] + at4 + h * 128, at, 0));
+    }
   };
-  f4 acc[TN][TM];
+  auto take_scales = [&]() {
 #pragma unroll
-  for (int i = 0; i < TN; ++i)
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-
-  auto multiply = [&](int half, int kc, auto sel) {
-    constexpr int SEL = decltype(sel)::value;
-    const uint8_t* base = lds + half * STAGE + kc * kChunkBytes + lane * 16;
-    i4v ca[TN], cb[TM];
+      for (int i = 0; i < TN; ++i) sa[i][h] = na[i][h];
 #pragma unroll
-    for (int j = 0; j < TM; ++j) cb[j] = *reinterpret_cast<const i4v*>(base + (RT + wm * TM + j) * KC * kChunkBytes);
-#pragma unroll
-    for (int i = 0; i < TN; ++i) ca[i] = *reinterpret_cast<const i4v*>(base + (wn * TN + i) * KC * kChunkBytes);
+      for (int j = 0; j < TM; ++j) sb[j][h] = nb[j][h];
+    }
+  };
+  i4v ca[2][TN][2], cb[2][TM];
+  auto weights = [&](int c, int to) {
+    const uint32_t at = chunk_at(c);
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
-      for (int j = 0; j < TM; ++j) acc[i][j] = mfma_mx<SEL, SEL>(ca[i], cb[j], acc[i][j], sa[i], sb[j]);
+      for (int h = 0; h < 2; ++h)
+        ca[to][i][h] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(i < PT ? wbuf0 : wbuf1, wo[i % PT] + at16 + h * 512, at, 0));
+    asm volatile("" ::: "memory");  // keeps the order of the loads: the waits below count them
   };
-  scales(0);
-  fetch(0, 0);
-  constexpr int STEPS = 4 / KC;
-  auto stage = [&](int rec, auto step) {
-    constexpr int S = decltype(step)::value;
-    const int c = rec * 4 + S * KC;
-    if (S > 0 && c >= chunks) return;  // the last record may be shorter
-    const int half = (rec * STEPS + S) & 1;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (S == 0) {
+  auto tokens = [&](int half, int c, int h) {  // half chunk 2 c + h of a record, to cb[h]
+    const uint8_t* base = lds + half * STAGE + (wm * TM * 8 + second * 4 + c) * kChunkBytes + at16 + h * 512;
 #pragma unroll
-      for (int i = 0; i < TN; ++i) sa[i] = na[i];
+    for (int j = 0; j < TM; ++j) cb[h][j] = *reinterpret_cast<const i4v*>(base + j * 8 * kChunkBytes);
+  };
+  f16v acc[TN][TM];
 #pragma unroll
-      for (int j = 0; j < TM; ++j) sb[j] = nb[j];
-      scales(rec + 1);
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  auto multiply = [&](auto which, auto half_chunk) {
+    constexpr int C = decltype(which)::value, H = decltype(half_chunk)::value;
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int i = 0; i < TN; ++i) acc[i][j] = mfma_mx32<C, C>(ca[C & 1][i][H], cb[H][j], acc[i][j], sa[i][H], sb[j][H]);
+  };
+  // One chunk: two halves, the second's and then the next chunk's token fragments read ahead of the products.
+  auto chunk = [&](int rec, int ring, auto which) {
+    constexpr int C = decltype(which)::value;
+    tokens(ring, C, 1);
+    __builtin_amdgcn_sched_barrier(0);  // as written: the scheduler would move the reads to their uses
+    multiply(which, std::integral_constant<int, 0>());
+    __builtin_amdgcn_sched_barrier(0);
+    if (C < 3) {
+      tokens(ring, C + 1, 0);
+    } else {
+      // The next record's tokens have arrived: their loads are older than the 2 TN latest, and than the last
+      // chunk's weights that the products above have waited for.  All waves are past their reads of this record.
+      __builtin_amdgcn_s_waitcnt(0x0070 | (2 * TN));  // vmcnt(2 TN) lgkmcnt(0)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      tokens(ring ^ 1, 0, 0);
     }
-    if (c + KC < chunks) fetch(c + KC, half ^ 1);
-    multiply(half, 0, std::integral_constant<int, S * KC>());
-    if (KC > 1 && c + 1 < chunks) multiply(half, 1, std::integral_constant<int, (S * KC + 1) & 3>());
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(which, std::integral_constant<int, 1>());
+    __builtin_amdgcn_sched_barrier(0);
+    weights(rec * 4 + C + 2, C & 1);
+    __builtin_amdgcn_sched_barrier(0);
   };
-  for (int rec = 0; rec < records; ++rec) {
-    stage(rec, std::integral_constant<int, 0>());
-    if (STEPS > 1) stage(rec, std::integral_constant<int, 1 % STEPS>());
-    if (STEPS > 2) stage(rec, std::integral_constant<int, 2 % STEPS>());
-    if (STEPS > 2) stage(rec, std::integral_constant<int, 3 % STEPS>());
+  fetch(0, 0);
+  scales(0);
+  asm volatile("" ::: "memory");
+  weights(0, 0);
+  weights(1, 1);
+  __builtin_amdgcn_s_waitcnt(0x0070);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  tokens(0, 0, 0);
+  const int whole = chunks / 4;
+  for (int rec = 0; rec < whole; ++rec) {
+    take_scales();
+    if (rec + 1 < records) fetch(rec + 1, (rec + 1) & 1);
+    scales(rec + 1);
+    asm volatile("" ::: "memory");
+    chunk(rec, rec & 1, std::integral_constant<int, 0>());
+    chunk(rec, rec & 1, std::integral_constant<int, 1>());
+    chunk(rec, rec & 1, std::integral_constant<int, 2>());
+    chunk(rec, rec & 1, std::integral_constant<int, 3>());
+  }
+  if (whole < records) {  // one to three chunks more
+    take_scales();
+    chunk(whole, whole & 1, std::integral_constant<int, 0>());
+    if (chunks - whole * 4 > 1) chunk(whole, whole & 1, std::integral_constant<int, 1>());
+    if (chunks - whole * 4 > 2) chunk(whole, whole & 1, std::integral_constant<int, 2>());
   }
 
+  auto out = [&](auto t, auto whole) {
 #pragma unroll
-  for (int j = 0; j < TM; ++j) {
-    const int token = (tbk * CT + wm * TM + j) * kRows + (lane & 15);
+    for (int j = 0; j < TM; ++j) {
+      const int token = (tbk * CT + wm * TM + j) * 32 + (lane & 31);
 #pragma unroll
-    for (int i = 0; i < PT; ++i) {
-      const int n0 = ((rb * WN + wn) * PT + i) * kRows + (lane >> 4) * 4;
-      finish<MODE>(a, token, n0, acc[i][j], acc[NM == 2 ? PT + i : i][j]);
+      for (int i = 0; i < PT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int n0 = ((rb * WN + wn) * PT + i) * 32 + r * 8 + (lane >> 5) * 4;
+          const f16v &v = acc[i][j], &u = acc[NM == 2 ? PT + i : i][j];
+          finish<MODE, typename decltype(t)::type, decltype(whole)::value>(
+              a, token, n0, f4{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]},
+              f4{u[4 * r], u[4 * r + 1], u[4 * r + 2], u[4 * r + 3]});
+        }
     }
-  }
+  };
+  const int type = MODE == kGatedGrad ? a.dh_type : a.y_type;
+  const bool all = (rb + 1) * (WN * PT * 32) <= a.n && (tbk + 1) * (CT * 32) <= a.m && (MODE == kGatedGrad ? a.dh_vec : a.y_vec);
+  auto typed = [&](auto t) { all ? out(t, std::true_type()) : out(t, std::false_type()); };
+  if (type == POLYQ_MX_BF16) typed(BF16());
+  else if (type == POLYQ_MX_F16) typed(F16());
+  else typed(F32());
 }
 
 // ---------------------------------------------------------------- launches
@@ -266,14 +324,14 @@ polyq_status run_stream(const Args& a, hipStream_t st) {
   return launched();
 }
 
-template <int MODE, int WN, int WM, int TN, int TM, int KC>
+template <int MODE, int WN, int WM, int TN, int TM>
 polyq_status run_gemm(Args a, hipStream_t st) {
   const int pt = WN * TN / (MODE == kLinear ? 1 : 2);
-  a.token_blocks = div_up(MODE == kGatedGrad ? a.m_pad / kRows : tiles_of(a.m), WM * TM);
-  const int64_t groups = static_cast<int64_t>(div_up(MODE == kGatedGrad ? a.n_pad / kRows : tiles_of(a.n), pt)) * a.token_blocks;
+  a.token_blocks = div_up(MODE == kGatedGrad ? a.m_pad : a.m, WM * TM * 32);
+  const int64_t groups = static_cast<int64_t>(div_up(MODE == kGatedGrad ? a.n_pad : a.n, pt * 32)) * a.token_blocks;
   if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
-  const size_t lds = 2 * static_cast<size_t>(WN * TN + WM * TM) * KC * kChunkBytes;
-  const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM, KC>;
+  const size_t lds = 16 * static_cast<size_t>(WM * TM) * kChunkBytes;
+  const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM>;
   if (lds > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(lds)) != hipSuccess)
@@ -286,8 +344,8 @@ template <int MODE>
 polyq_status run(const Args& a, hipStream_t st) {
   if (MODE != kGatedGrad && a.m <= 16) return run_stream<MODE, MODE == kLinear ? 1 : 2, 1, 8>(a, st);
   const int64_t tiles = static_cast<int64_t>(tiles_of(a.n)) * (MODE == kLinear ? 1 : 2) * tiles_of(a.m);
-  if (tiles >= 256 * 256) return run_gemm<MODE, 2, 4, 8, 4, 2>(a, st);
-  return run_gemm<MODE, 2, 2, 4, 4, 2>(a, st);
+  if (tiles >= 128 * 128) return run_gemm<MODE, 4, 1, 2, 4>(a, st);
+  return run_gemm<MODE, 4, 1, 2, 2>(a, st);
 }
 
 }  // namespace

@@ -1,12 +1,10 @@
 // Gradients through products of microscaled 4-bit matrices.
 //
-// Both are products C[p][c] = sum_r A[p][r] B[r][c] whose right operand is a packed
-// matrix with the reduction along its ROWS:
-//   dx[t][c]  = sum_n d[t][n] W[n][c]     (A = d,    B = W;  gated: dg, G and du, U in one sum)
-//   dW[n][c]  = sum_t d[t][n] x^[t][c]    (A = d^T,  B = x^)
-// The blocks' scales run along c, so they do not factor out of the sum over r and the 4-bit
-// matrix instructions do not apply: B is converted to bf16 (exact: two significant bits
-// and a power of two) on its way into LDS and multiplied on the bf16 matrix cores.  A
+//   dx[t][c]  = sum_n d[t][n] W[n][c]     (gated: dg, G and du, U in one sum)
+//   dW[n][c]  = sum_t d[t][n] x^[t][c]
+// The blocks' scales run along c, so they do not factor out of the sums and the 4-bit
+// matrix instructions do not apply: W and x^ are converted to bf16 (exact: two
+// significant bits and a power of two) and multiplied on the bf16 matrix cores.  d
 // comes as planes of bf16 terms whose sum is the value (launch_gated_grad): one term for
 // gradients in bf16 (an error of 2^-9 per factor, as large as the result's own rounding),
 // two for fp16, three for fp32.
@@ -21,210 +19,295 @@ namespace polyq {
 namespace mx {
 namespace {
 
-constexpr int kStep = 64;  // rows of the reduction per stage
+// A gradient product of either kind is D[l][s] = sum_r L[r][l] S[s][r]:
+//   dx   l = c, s = t, r = n:  L = W, converted;           S = d
+//   dW   l = n, s = c, r = t:  L = d;                      S = x^ transposed, converted once
+// L passes through LDS in blocks of 32 r x 16 l (1 KiB, rows of 32 bytes) and is read transposed;
+// S is stored in memory as blocks of 32 s x 16 r, which are the operand fragments of a
+// wave, and goes from there into registers.
+constexpr int kStep = 64;            // r of a stage
+constexpr int kBlockBytes = 1024;    // 32 x 16 bf16
+constexpr int kMaxRows = 1 << 21;    // tokens and output channels: a work-group's S is reached with 32-bit offsets
 
 struct GradArgs {
-  const __bf16* a;      // planes [terms][a_rows][mats][a_pitch]
-  const uint8_t* b[2];  // packed matrices
-  void* c[2];           // outputs [p][k]
-  float* part;          // splits > 1: [splits][outputs][p][k]
-  int64_t plane;        // elements of a plane
-  int64_t row;          // elements from one plane row to the next: mats * pitch
-  int32_t pitch;        // a_pitch
-  int32_t mats;         // matrices: summed over (dx) or one output each (dW)
-  int32_t p, k;         // of an output
-  int32_t p_pad;        // p of the planes (a multiple of 64)
-  int32_t b_rows;       // rows of each packed matrix
-  int32_t rsteps;       // stages of one (term, matrix)
-  int32_t terms, splits;
+  const uint8_t* d;     // planes [terms][mats][p_tiles][n_tiles] of blocks of 32 tokens x 16 n
+  const uint8_t* xt;    // dW: [c_tiles][m_tiles] blocks of 32 c x 16 tokens
+  const uint8_t* w[2];  // dx: the packed weights
+  void* out[2];         // dx [m][k]; dW [n][k] each
+  float* part;          // splits > 1: [splits][outputs][rows][k]
+  int64_t plane;        // bytes of the planes of one term and matrix
+  int32_t mats, terms, splits;
+  int32_t m, n, k;
+  int32_t m_pad, n_pad; // multiples of 64
+  int32_t rows;         // of an output: m or n
+  int32_t rsteps;       // stages of one term (and matrix)
+  int32_t l_blocks, s_blocks;
   int32_t type, vec;    // of the outputs; rows take vector accesses of four elements
-  int32_t p_blocks, c_blocks;
 };
 
-// 16-byte unit swizzles: see the kernel.
-__device__ __forceinline__ int row_swizzle(int r) { return (r & 3) | ((r >> 1) & 4); }
-
-// WP x WC waves, each TP tiles of 16 p by TC tiles of 16 c.  TRANS: the planes hold A
-// transposed (their rows are the reduction).
-template <bool TRANS, int WP, int WC, int TP, int TC>
-__global__ __launch_bounds__(64 * WP * WC) void mx_grad_kernel(const GradArgs g) {
-  constexpr int W = WP * WC, P = WP * TP * 16, C = WC * TC * 16;
-  constexpr int A_BYTES = P * kStep * 2, B_BYTES = C * kStep * 2, STAGE = A_BYTES + B_BYTES;
-  constexpr int A_LOADS = A_BYTES / 1024 / W;           // 1 KiB pieces of a wave
-  constexpr int B_FRAGS = (C / kChunk) * (kStep / kRows);  // packed fragments of a stage
-  constexpr int B_LOADS = B_FRAGS / W;
-  static_assert(A_LOADS * W * 1024 == A_BYTES && B_LOADS * W == B_FRAGS && C % kChunk == 0, "tile");
+// WL x WS waves, each TL x 32 l by TS x 32 s.
+template <bool DW, int WL, int WS, int TL, int TS>
+__global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs g) {
+  constexpr int W = WL * WS, L = WL * TL * 32, S = WS * TS * 32;
+  constexpr int STAGE = L * kStep * 2;
+  constexpr int DMA = STAGE / kBlockBytes / W;                    // dW: blocks a wave fetches per stage
+  constexpr int FRAGS = (L / kChunk) * (kStep / kRows) / W;       // dx: packed fragments a wave converts per stage
+  static_assert(DMA * W * kBlockBytes == STAGE && FRAGS * W * kChunk * kRows == L * kStep && L % kChunk == 0, "tile");
   extern __shared__ uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wp = wave % WP, wc = wave / WP;
+  const int wl = wave % WL, ws = wave / WL;
   const int total = static_cast<int>(gridDim.x), per = total / 8, rest = total % 8;
   const int xcd = static_cast<int>(blockIdx.x) % 8, turn = static_cast<int>(blockIdx.x) / 8;
   int id = xcd * per + min(xcd, rest) + turn;
-  const int pb = id % g.p_blocks;
-  id /= g.p_blocks;
-  const int cb = id % g.c_blocks;
-  const int out = id / g.c_blocks;  // the output matrix (dW)
-  const int p0 = pb * P, chunk0 = cb * (C / kChunk);
-  const int chunks = chunks_of(g.k), b_tiles = tiles_of(g.b_rows);
+  const int sb = id % g.s_blocks;
+  id /= g.s_blocks;
+  const int lb = id % g.l_blocks, mat_out = id / g.l_blocks;  // the output matrix (dW)
   const int64_t tb = tile_bytes(g.k);
 
-  // Stages: terms x (TRANS ? 1 : mats) x rsteps, split evenly.
-  const int inner = TRANS ? g.rsteps : g.rsteps * g.mats;
-  const int stages = inner * g.terms;
-  const int s0 = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / g.splits);
-  const int s1 = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / g.splits);
+  // Stages: terms x (DW ? 1 : mats) x rsteps, split evenly.
+  const int stages = g.terms * g.rsteps * (DW ? 1 : g.mats);
+  const int first = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / g.splits);
+  const int last = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / g.splits);
 
-  auto fetch_a = [&](int s, int half) {
-    const int term = s / inner, r = s % inner;
-    const int mat = TRANS ? out : r / g.rsteps, r0 = (TRANS ? r : r % g.rsteps) * kStep;
-    const __bf16* base = g.a + term * g.plane + static_cast<int64_t>(mat) * g.pitch;
+  // S: fragments of the work-group's s tiles; r in tiles of 16.
+  const int s_tiles = DW ? div_up(g.k, 32) : g.m_pad / 32;
+  const int64_t s_tile = static_cast<int64_t>(DW ? g.m_pad : g.n_pad) / 16 * kBlockBytes;
+  const int s0 = min(sb * (S / 32), s_tiles - 1);
+  uint32_t so[TS];
 #pragma unroll
-    for (int i = 0; i < A_LOADS; ++i) {
-      const int piece = (i * W + wave) * 64 + lane;  // 16-byte piece of the stage, in LDS order
-      const __bf16* src;
-      if (TRANS) {  // rows of P elements: pieces swizzled in pairs (32 bytes, a tile of 16 p)
-        const int r16 = piece / (P / 8), slot = piece % (P / 8);
-        const int pc = ((slot >> 1) ^ row_swizzle(r16)) * 2 + (slot & 1);
-        src = base + static_cast<int64_t>(r0 + r16) * g.row + min(p0 + pc * 8, g.p_pad - 8);
-      } else {  // rows of 64 elements = 8 pieces
-        const int row = piece >> 3, pc = (piece & 7) ^ (row & 7);
-        src = base + static_cast<int64_t>(min(p0 + row, g.p_pad - 1)) * g.row + r0 + pc * 8;
-      }
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                       (__attribute__((address_space(3))) void*)(lds + half * STAGE + (i * W + wave) * 1024),
-                                       16, 0, 0);
+  for (int i = 0; i < TS; ++i)
+    so[i] = static_cast<uint32_t>(min(sb * (S / 32) + ws * TS + i, s_tiles - 1) - s0) * static_cast<uint32_t>(s_tile) +
+            (lane & 31) * 32 + (lane >> 5) * 16;
+  i4v sf[4][TS];
+  auto load_s = [&](int stage, auto which) {  // the fragments of step J of a stage (the last one again past the end)
+    constexpr int J = decltype(which)::value;
+    const int st = min(stage, last - 1), r = st % g.rsteps, plane = st / g.rsteps;
+    const uint8_t* base = (DW ? g.xt : g.d + plane * g.plane) + s0 * s_tile;
+    const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, (s_tiles - s0) * s_tile);
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+      sf[J][i] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(buf, so[i], (r * 4 + J) * kBlockBytes, 0));
+  };
+
+  // L of dW: blocks straight into LDS.
+  const int n_tiles = g.n_pad / 16;
+  auto fetch = [&](int stage, int half) {
+    const int r = stage % g.rsteps, plane = stage / g.rsteps * g.mats + mat_out;
+    const int n0 = min(lb * (L / 16), n_tiles - 1);
+    const uint8_t* base = g.d + plane * g.plane + (static_cast<int64_t>(r) * 2 * n_tiles + n0) * kBlockBytes;
+    const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, (static_cast<int64_t>(2) * n_tiles - n0) * kBlockBytes);
+#pragma unroll
+    for (int i = 0; i < DMA; ++i) {
+      const int block = i * W + wave, rt = block / (L / 16), lt = min(lb * (L / 16) + block % (L / 16), n_tiles - 1) - n0;
+      load_to_lds(buf, lds + half * STAGE + block * kBlockBytes, lane * 16, (rt * n_tiles + lt) * kBlockBytes);
     }
   };
-  i4v codes[B_LOADS];
-  uint32_t bytes[B_LOADS];
-  auto fetch_b = [&](int s) {
-    const int r = s % inner;
-    const int mat = TRANS ? 0 : r / g.rsteps, t0 = (TRANS ? r : r % g.rsteps) * (kStep / kRows);
+  // L of dx: packed fragments (16 r x 128 l) into registers, and from there as bf16 into LDS.
+  const int chunks = chunks_of(g.k), b_tiles = tiles_of(g.n);
+  i4v codes[FRAGS];
+  uint32_t bytes[FRAGS];
+  auto fetch_codes = [&](int stage) {
+    const int st = min(stage, last - 1), r = st % g.rsteps, mat = st / g.rsteps % g.mats;
 #pragma unroll
-    for (int i = 0; i < B_LOADS; ++i) {
-      const int f = i * W + wave, tile = t0 + f % (kStep / kRows), c = min(chunk0 + f / (kStep / kRows), chunks - 1);
-      const uint8_t* src = g.b[mat] + min(tile, b_tiles - 1) * tb;
+    for (int i = 0; i < FRAGS; ++i) {
+      const int f = i * W + wave, tile = r * (kStep / kRows) + f % (kStep / kRows);
+      const int c = min(lb * (L / kChunk) + f / (kStep / kRows), chunks - 1);
+      const uint8_t* src = (mat ? g.w[1] : g.w[0]) + min(tile, b_tiles - 1) * tb;
       codes[i] = *reinterpret_cast<const i4v*>(src + chunk_offset(c) + lane * 16);
       bytes[i] = src[scale_offset(c) + lane * 4 + (c & 3)];
       if (tile >= b_tiles) codes[i] = i4v{0, 0, 0, 0}, bytes[i] = 127;  // rows behind the last: zeros
     }
   };
-  auto store_b = [&](int half) {
-    uint8_t* base = lds + half * STAGE + A_BYTES;
+  auto convert = [&](int half, auto which) {  // half H of each fragment's 32 channels per lane
+    constexpr int H = decltype(which)::value;
 #pragma unroll
-    for (int i = 0; i < B_LOADS; ++i) {
-      const int f = i * W + wave, r = (f % (kStep / kRows)) * kRows + (lane & 15);
-      const int unit = (f / (kStep / kRows)) * 8 + (lane >> 4) * 2;  // 32-byte units of 16 columns
+    for (int i = 0; i < FRAGS; ++i) {
+      const int f = i * W + wave, rt = f % (kStep / kRows);
       const float s = scale_value(bytes[i]);
-      const bool nan = bytes[i] == kNanScale;
+      uint32_t v[8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t v[8];
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint32_t code = static_cast<uint32_t>(codes[i][h * 2 + w]);
-          v[w * 4 + 0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0));
-          v[w * 4 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1));
-          v[w * 4 + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2));
-          v[w * 4 + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3));
-        }
-        if (nan) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = 0x7fc07fc0u;
-        }
-        uint8_t* dst = base + r * (C * 2) + ((unit + h) ^ row_swizzle(r)) * 32;
-        *reinterpret_cast<u4v*>(dst) = u4v{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<u4v*>(dst + 16) = u4v{v[4], v[5], v[6], v[7]};
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t code = static_cast<uint32_t>(codes[i][H * 2 + w]);
+        v[w * 4 + 0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0));
+        v[w * 4 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1));
+        v[w * 4 + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2));
+        v[w * 4 + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3));
       }
-    }
-  };
-  // Fragment of a 64-row tile in LDS with the reduction along its rows: 8 rows (32 s + 8 (lane /
-  // 16) ..) of column lane % 16 of unit `unit`.  A transposing read hands lane j of 16
-  // lanes column j of the four rows whose 32 bytes those lanes address.
-  auto frag_rows = [&](const uint8_t* base, int pitch, int s, int unit) -> bf16x8 {
-    const int i = lane & 15, r = s * 32 + (lane >> 4) * 8 + (i >> 2);
-    typedef short s4 __attribute__((ext_vector_type(4)));
-    union {
-      s4 h[2];
-      bf16x8 v;
-    } u;
+      if (bytes[i] == kNanScale) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = r + 4 * h;
-      const uint8_t* p = base + row * pitch + (unit ^ row_swizzle(row)) * 32 + (i & 3) * 8;
-      u.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(p));
-    }
-    return u.v;
-  };
-  f4 acc[TP][TC];
-#pragma unroll
-  for (int i = 0; i < TP; ++i)
-#pragma unroll
-    for (int j = 0; j < TC; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-  auto multiply = [&](int half) {
-    const uint8_t* la = lds + half * STAGE;
-    const uint8_t* lb = la + A_BYTES;
-#pragma unroll
-    for (int s = 0; s < kStep / 32; ++s) {
-      bf16x8 fa[TP], fb[TC];
-#pragma unroll
-      for (int j = 0; j < TC; ++j) fb[j] = frag_rows(lb, C * 2, s, wc * TC + j);
-#pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        if (TRANS) {
-          fa[i] = frag_rows(la, P * 2, s, wp * TP + i);
-        } else {
-          const int row = (wp * TP + i) * 16 + (lane & 15), pc = (s * 4 + (lane >> 4)) ^ (row & 7);
-          fa[i] = *reinterpret_cast<const bf16x8*>(la + row * (kStep * 2) + pc * 16);
-        }
+        for (int j = 0; j < 8; ++j) v[j] = 0x7fc07fc0u;
       }
-#pragma unroll
-      for (int i = 0; i < TP; ++i)
-#pragma unroll
-        for (int j = 0; j < TC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      const int lt = f / (kStep / kRows) * 8 + (lane >> 4) * 2 + H;
+      uint8_t* dst = lds + half * STAGE + ((rt >> 1) * (L / 16) + lt) * kBlockBytes + ((rt & 1) * 16 + (lane & 15)) * 32;
+      *reinterpret_cast<u4v*>(dst) = u4v{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<u4v*>(dst + 16) = u4v{v[4], v[5], v[6], v[7]};
     }
   };
-  if (s0 < s1) {
-    fetch_a(s0, 0);
-    fetch_b(s0);
-    store_b(0);
-    if (s0 + 1 < s1) fetch_b(s0 + 1);
-  }
-  for (int s = s0; s < s1; ++s) {
-    const int half = (s - s0) & 1;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
+  // Fragment of 32 l x 16 r: a transposing read hands lane j of 16 lanes column j of the four rows whose 32
+  // bytes those lanes address; lane groups 1 and 3 have l 16 .. 31, groups 2 and 3 r 8 .. 15.
+  const int l_lane = ((lane >> 4) & 1) * kBlockBytes + ((lane >> 5) * 8 + ((lane & 15) >> 2)) * 32 + (lane & 3) * 8;
+  bf16x8 lf[2][TL];
+  auto read_l = [&](int half, int step, int to) {
+    const uint8_t* base = lds + half * STAGE + ((step >> 1) * (L / 16) + wl * TL * 2) * kBlockBytes + (step & 1) * 512 + l_lane;
+#pragma unroll
+    for (int i = 0; i < TL; ++i) lf[to][i] = read_transposed(base + i * 2 * kBlockBytes);
+  };
+
+  f16v acc[TL][TS];
+#pragma unroll
+  for (int i = 0; i < TL; ++i)
+#pragma unroll
+    for (int j = 0; j < TS; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  auto multiply = [&](auto which) {  // rows of D: the output's columns c
+    constexpr int J = decltype(which)::value;
+#pragma unroll
+    for (int j = 0; j < TS; ++j) {
+      const bf16x8 sv = __builtin_bit_cast(bf16x8, sf[J][j]);
+#pragma unroll
+      for (int i = 0; i < TL; ++i)
+        acc[i][j] = DW ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(sv, lf[J & 1][i], acc[i][j], 0, 0, 0)
+                       : __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf[J & 1][i], sv, acc[i][j], 0, 0, 0);
+    }
+  };
+  typedef std::integral_constant<int, 0> I0;
+  typedef std::integral_constant<int, 1> I1;
+  typedef std::integral_constant<int, 2> I2;
+  typedef std::integral_constant<int, 3> I3;
+  auto fence = [&]() {
     asm volatile("" ::: "memory");
-    if (s + 1 < s1) {
-      store_b(half ^ 1);
-      fetch_a(s + 1, half ^ 1);
-      if (s + 2 < s1) fetch_b(s + 2);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (first < last) {
+    if (DW) {
+      fetch(first, 0);
+    } else {
+      fetch_codes(first);
+      convert(0, I0());
+      convert(0, I1());
+      fetch_codes(first + 1);
     }
-    multiply(half);
+    load_s(first, I0());
+    load_s(first, I1());
+    load_s(first, I2());
+    load_s(first, I3());
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();
+    fence();
+    read_l(0, 0, 0);
   }
-#pragma unroll
-  for (int i = 0; i < TP; ++i) {
-    const int row = p0 + (wp * TP + i) * 16 + (lane & 15);
-    if (row >= g.p) continue;
-#pragma unroll
-    for (int j = 0; j < TC; ++j) {
-      const int col = cb * C + (wc * TC + j) * 16 + (lane >> 4) * 4;
-      if (col >= g.k) continue;
-      const int64_t at = static_cast<int64_t>(row) * g.k + col;
-      if (g.splits > 1) {
-        const int outs = TRANS ? g.mats : 1;
-        float* part = g.part + (static_cast<int64_t>(blockIdx.y) * outs + out) * g.p * g.k;
-        store4(part + at, acc[i][j], g.k % 4 == 0, g.k - col);
-      } else {
-        store4(g.c[out], g.type, at, acc[i][j], g.vec, g.k - col);
-      }
+  for (int stage = first; stage < last; ++stage) {
+    const int half = (stage - first) & 1;
+    // The other half is free: every wave read the last of it before the barrier below.
+    if (DW && stage + 1 < last) fetch(stage + 1, half ^ 1);
+    fence();
+    read_l(half, 1, 1);
+    fence();
+    multiply(I0());
+    fence();
+    load_s(stage + 1, I0());
+    if (!DW) convert(half ^ 1, I0());
+    fence();
+    read_l(half, 2, 0);
+    fence();
+    multiply(I1());
+    fence();
+    load_s(stage + 1, I1());
+    if (!DW) {
+      convert(half ^ 1, I1());
+      fetch_codes(stage + 2);
     }
+    fence();
+    read_l(half, 3, 1);
+    fence();
+    multiply(I2());
+    fence();
+    load_s(stage + 1, I2());
+    fence();
+    // The next stage's L is in LDS: dW's own loads are older than the 3 TS of S since.
+    if (DW)
+      __builtin_amdgcn_s_waitcnt(0x0070 | (3 * TS & 15) | (3 * TS >> 4 << 14));
+    else
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    fence();
+    read_l(half ^ 1, 0, 0);
+    fence();
+    multiply(I3());
+    fence();
+    load_s(stage + 1, I3());
+  }
+  const bool vec = g.splits > 1 ? g.k % 4 == 0 : g.vec;
+  auto out = [&](auto t) {
+    typedef typename decltype(t)::type T;
+    T* base = static_cast<T*>(g.splits > 1 ? static_cast<void*>(g.part + (static_cast<int64_t>(blockIdx.y) * (DW ? g.mats : 1) + mat_out) *
+                                                                              g.rows * g.k)
+                                           : (mat_out ? g.out[1] : g.out[0]));
+#pragma unroll
+    for (int i = 0; i < TL; ++i)
+#pragma unroll
+      for (int j = 0; j < TS; ++j) {
+        const int lt = (lb * WL + wl) * TL + i, st = (sb * WS + ws) * TS + j;
+        const int row = (DW ? lt : st) * 32 + (lane & 31), col = (DW ? st : lt) * 32 + (lane >> 5) * 4;
+        if (row >= g.rows) continue;
+        T* to = base + static_cast<int64_t>(row) * g.k + col;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (col + r * 8 < g.k)
+            store4(to + r * 8, f4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]}, vec,
+                   g.k - col - r * 8);
+      }
+  };
+  if (g.splits > 1 || g.type == POLYQ_MX_F32) out(F32());
+  else if (g.type == POLYQ_MX_F16) out(F16());
+  else out(BF16());
+}
+
+// x^ [m][k], packed, as bf16 blocks of 32 channels x 16 tokens, [c_tiles][m_pad / 16], zero
+// behind m and k.  A wave takes a chunk of a tile: its lanes convert 32 values each into LDS,
+// 4 blocks of 16 tokens x 32 channels, and read them transposed.
+__global__ __launch_bounds__(256) void mx_transpose_kernel(const uint8_t* __restrict__ packed, uint8_t* __restrict__ out, int m,
+                                                           int k, int m_tiles, int c_tiles, int64_t jobs) {
+  __shared__ uint8_t lds[4][4 * kBlockBytes];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+  if (job >= jobs) return;  // waves are independent: no barrier follows
+  const int chunks = chunks_of(k), tile = static_cast<int>(job / chunks), chunk = static_cast<int>(job % chunks);
+  const bool there = tile * kRows < m;
+  const uint8_t* src = packed + min(tile, tiles_of(m) - 1) * tile_bytes(k);
+  const i4v codes = *reinterpret_cast<const i4v*>(src + chunk_offset(chunk) + lane * 16);
+  const uint32_t byte = src[scale_offset(chunk) + lane * 4 + (chunk & 3)];
+  const float s = scale_value(byte);
+  uint8_t* block = lds[wave] + (lane >> 4) * kBlockBytes;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t code = static_cast<uint32_t>(codes[w]);
+    u4v v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)),
+             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
+             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
+             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
+    if (byte == kNanScale) v = u4v{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    if (!there) v = u4v{0, 0, 0, 0};
+    *reinterpret_cast<u4v*>(block + (lane & 15) * 64 + w * 16) = v;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // Lane group h = lane / 16 of a block: channels 16 (h & 1) .. + 15, tokens 8 (h >> 1) .. + 7.
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int ct = chunk * 4 + q;
+    const int i = lane & 15;
+    const uint8_t* p = lds[wave] + q * kBlockBytes + ((lane >> 5) * 8 + (i >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
+    const bf16x8 v = read_transposed(p, 4 * 64);
+    if (ct < c_tiles)
+      *reinterpret_cast<bf16x8*>(out + (static_cast<int64_t>(ct) * m_tiles + tile) * kBlockBytes + (((lane >> 4) & 1) * 16 + i) * 32 +
+                                 (lane >> 5) * 16) = v;
   }
 }
 
 // Adds the splits' sums in order.
 __global__ __launch_bounds__(256) void mx_grad_sum_kernel(const GradArgs g) {
-  const int64_t n = static_cast<int64_t>(g.p) * g.k;
+  const int64_t n = static_cast<int64_t>(g.rows) * g.k;
   const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
   if (at >= n) return;
   const int valid = static_cast<int>(min(static_cast<int64_t>(4), n - at));
@@ -232,78 +315,75 @@ __global__ __launch_bounds__(256) void mx_grad_sum_kernel(const GradArgs g) {
   const bool vec = n % 4 == 0;
   f4 v = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < g.splits; ++s) v += load4(g.part + (static_cast<int64_t>(s) * outs + out) * n + at, vec, valid);
-  store4(g.c[out], g.type, at, v, g.vec, valid);
+  store4(out ? g.out[1] : g.out[0], g.type, at, v, g.vec, valid);
 }
 
-// d [m][n] into planes of bf16 terms [terms][m_pad][n_pad], zero in the padding: four elements a thread.
+// d [m][n] into the planes, zero in the padding: four elements a thread.
 __global__ __launch_bounds__(256) void mx_planes_kernel(const void* __restrict__ d, int type, int m, int n, int vec,
-                                                        __bf16* __restrict__ planes, int terms, int m_pad, int n_pad) {
-  const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (at >= static_cast<int64_t>(m_pad) * n_pad) return;
-  const int row = static_cast<int>(at / n_pad), col = static_cast<int>(at % n_pad);
+                                                        uint8_t* __restrict__ planes, int terms, int m_pad, int n_pad) {
+  const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (id >= static_cast<int64_t>(m_pad) * n_pad / 4) return;
+  const int row = static_cast<int>(id / (n_pad / 4)), col = static_cast<int>(id % (n_pad / 4)) * 4;
   f4 v = {0.f, 0.f, 0.f, 0.f};
   if (row < m && col < n) v = load4(d, type, static_cast<int64_t>(row) * n + col, vec, n - col);
-  for (int t = 0; t < terms; ++t) {
-    const bf16x4 b = next_terms(&v);
-    *reinterpret_cast<bf16x4*>(planes + static_cast<int64_t>(t) * m_pad * n_pad + at) = b;
-  }
+  for (int t = 0; t < terms; ++t)
+    *reinterpret_cast<bf16x4*>(planes + t * (static_cast<int64_t>(m_pad) * n_pad * 2) + plane_at(row, col, n_pad)) = next_terms(&v);
 }
 
 polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
 
 inline int64_t pad64(int64_t v) { return align_up(v, 64); }
 
-// One gradient product's tile and splits.
+// One gradient product's tile and splits: outputs of `l` by `s`, `stages` of the reduction.
 struct Shape {
   bool big;
-  int p_blocks, c_blocks, splits;
+  int l_blocks, s_blocks, splits;
 };
-Shape grad_shape(int p, int k, int outs, int stages) {
-  Shape s;
-  const int64_t big = static_cast<int64_t>(div_up(p, 256)) * div_up(k, 256) * outs;
-  s.big = big >= 200;
-  const int tile = s.big ? 256 : 128;
-  s.p_blocks = div_up(p, tile), s.c_blocks = div_up(k, tile);
-  const int64_t groups = static_cast<int64_t>(s.p_blocks) * s.c_blocks * outs;
+Shape grad_shape(int l, int s, int outs, int stages) {
+  Shape h;
+  const int64_t big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs;
+  h.big = big >= 128;
+  h.l_blocks = div_up(l, 256), h.s_blocks = div_up(s, h.big ? 256 : 64);
+  const int64_t groups = static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs;
   // Split the reduction where the output's tiles leave most of the GPU idle: at least 8 stages each.
-  s.splits = 1;
-  while (groups * s.splits * 2 <= 512 && stages / (s.splits * 2) >= 8 && s.splits < 32) s.splits *= 2;
-  return s;
+  h.splits = 1;
+  while (groups * h.splits * 2 <= 512 && stages / (h.splits * 2) >= 8 && h.splits < 32) h.splits *= 2;
+  return h;
 }
 
-template <bool TRANS, int WP, int WC, int TP, int TC>
+template <bool DW, int WL, int WS, int TL, int TS>
 polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
-  const size_t lds = 2 * static_cast<size_t>(WP * TP * 16 + WC * TC * 16) * kStep * 2;
-  const auto kernel = mx_grad_kernel<TRANS, WP, WC, TP, TC>;
+  const size_t lds = 2 * static_cast<size_t>(WL * TL * 32) * kStep * 2;
+  const auto kernel = mx_grad_kernel<DW, WL, WS, TL, TS>;
   if (lds > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(lds)) != hipSuccess)
     return POLYQ_ERR_DEVICE;
-  const int64_t groups = static_cast<int64_t>(g.p_blocks) * g.c_blocks * outs;
+  const int64_t groups = static_cast<int64_t>(g.l_blocks) * g.s_blocks * outs;
   if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
-  kernel<<<dim3(static_cast<uint32_t>(groups), g.splits), dim3(64 * WP * WC), lds, st>>>(g);
+  kernel<<<dim3(static_cast<uint32_t>(groups), g.splits), dim3(64 * WL * WS), lds, st>>>(g);
   return launched();
 }
 
-template <bool TRANS>
-polyq_status run_grad(GradArgs g, int outs, void* part, hipStream_t st) {
-  const int stages = g.terms * g.rsteps * (TRANS ? 1 : g.mats);
-  const Shape s = grad_shape(g.p, g.k, outs, stages);
-  g.splits = s.splits, g.p_blocks = s.p_blocks, g.c_blocks = s.c_blocks;
+template <bool DW>
+polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
+  const int outs = DW ? g.mats : 1, stages = g.terms * g.rsteps * (DW ? 1 : g.mats);
+  const Shape h = DW ? grad_shape(g.n, g.k, outs, stages) : grad_shape(g.k, g.m, outs, stages);
+  g.splits = h.splits, g.l_blocks = h.l_blocks, g.s_blocks = h.s_blocks;
   g.part = static_cast<float*>(part);
-  const polyq_status r = s.big ? run_tile<TRANS, 2, 4, 8, 4>(g, outs, st) : run_tile<TRANS, 2, 2, 4, 4>(g, outs, st);
-  if (r != POLYQ_OK || s.splits == 1) return r;
-  const int64_t blocks = (static_cast<int64_t>(g.p) * g.k + 1023) / 1024;
+  const polyq_status r = h.big ? run_tile<DW, 2, 4, 4, 2>(g, outs, st) : run_tile<DW, 4, 1, 2, 2>(g, outs, st);
+  if (r != POLYQ_OK || h.splits == 1) return r;
+  const int64_t blocks = (static_cast<int64_t>(g.rows) * g.k + 1023) / 1024;
   mx_grad_sum_kernel<<<dim3(static_cast<uint32_t>(blocks), outs), dim3(256), 0, st>>>(g);
   return launched();
 }
 
-// Workspace of a backward call, in order: packed x, planes, partial sums (of dx, then of the weights' gradients:
+// Workspace of a backward call, in order: packed x, planes, transposed x, partial sums (of dx, then of the weights' gradients:
 // one room, the launches are ordered).
 struct GradPlan {
   int terms;
   int32_t m_pad, n_pad;
-  size_t x_bytes, plane_bytes, part_bytes, total;
+  size_t x_bytes, plane_bytes, xt_bytes, part_bytes, total;
 };
 GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int grad_type, bool dx, bool dw) {
   GradPlan p;
@@ -311,16 +391,17 @@ GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int gr
   p.m_pad = static_cast<int32_t>(pad64(m)), p.n_pad = static_cast<int32_t>(pad64(n));
   p.x_bytes = x_type == POLYQ_MX_PACKED ? 0 : align_up(static_cast<int64_t>(polyq_mx_bytes(m, k)), 256);
   p.plane_bytes = static_cast<size_t>(p.terms) * p.m_pad * mats * p.n_pad * 2;
+  p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
   p.part_bytes = 0;
   if (dx) {
-    const Shape s = grad_shape(m, k, 1, p.terms * mats * (p.n_pad / kStep));
+    const Shape s = grad_shape(k, m, 1, p.terms * mats * (p.n_pad / kStep));
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * m * k * 4);
   }
   if (dw) {
     const Shape s = grad_shape(n, k, mats, p.terms * (p.m_pad / kStep));
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * mats * n * k * 4);
   }
-  p.total = p.x_bytes + p.plane_bytes + p.part_bytes;
+  p.total = p.x_bytes + p.plane_bytes + p.xt_bytes + p.part_bytes;
   return p;
 }
 
@@ -342,6 +423,7 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
   if (need_x && (q.x == nullptr || !(float_type(q.x_type) || q.x_type == POLYQ_MX_PACKED))) return POLYQ_ERR_ARG;
   if (q.m < 1) return POLYQ_ERR_ARG;
   if (!valid_shape(q.m, q.k) || !valid_shape(q.n, q.k)) return POLYQ_ERR_SHAPE;
+  if (q.m > kMaxRows || q.n > kMaxRows) return POLYQ_ERR_CAPACITY;
   if (!aligned(q.w[0], 256) || !aligned(q.w[1], 256) || !aligned(q.d, type_bytes(q.d_type))) return POLYQ_ERR_ARG;
   if (need_x && !aligned(q.x, q.x_type == POLYQ_MX_PACKED ? 256 : type_bytes(q.x_type))) return POLYQ_ERR_ARG;
   const int size = type_bytes(q.grad_type);
@@ -357,7 +439,8 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
     x = at;
   }
   void* planes = at + p.x_bytes;
-  void* part = at + p.x_bytes + p.plane_bytes;
+  uint8_t* xt = at + p.x_bytes + p.plane_bytes;
+  void* part = xt + p.xt_bytes;
   if (q.act >= 0) {
     const polyq_status s = launch_gated_grad(q.w[0], q.w[1], x, q.d, q.d_type, q.m, q.n, q.k, q.act, planes, p.terms,
                                              p.m_pad, p.n_pad, st);
@@ -367,26 +450,32 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
     if (blocks > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
     const int vec = q.n % 4 == 0 && aligned(q.d, 4 * type_bytes(q.d_type));
     mx_planes_kernel<<<dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st>>>(
-        q.d, q.d_type, q.m, q.n, vec, static_cast<__bf16*>(planes), p.terms, p.m_pad, p.n_pad);
+        q.d, q.d_type, q.m, q.n, vec, static_cast<uint8_t*>(planes), p.terms, p.m_pad, p.n_pad);
     const polyq_status s = launched();
     if (s != POLYQ_OK) return s;
   }
   GradArgs g{};
-  g.a = static_cast<const __bf16*>(planes);
-  g.mats = q.mats, g.pitch = p.n_pad, g.row = static_cast<int64_t>(q.mats) * p.n_pad, g.plane = g.row * p.m_pad;
-  g.k = q.k, g.terms = p.terms, g.type = q.grad_type;
+  g.d = static_cast<const uint8_t*>(planes), g.xt = xt;
+  g.w[0] = static_cast<const uint8_t*>(q.w[0]), g.w[1] = static_cast<const uint8_t*>(q.w[1]);
+  g.plane = static_cast<int64_t>(p.m_pad) * p.n_pad * 2;
+  g.mats = q.mats, g.terms = p.terms, g.type = q.grad_type;
+  g.m = q.m, g.n = q.n, g.k = q.k, g.m_pad = p.m_pad, g.n_pad = p.n_pad;
   if (q.dx != nullptr) {
-    g.b[0] = static_cast<const uint8_t*>(q.w[0]), g.b[1] = static_cast<const uint8_t*>(q.w[1]);
-    g.c[0] = q.dx, g.p = q.m, g.p_pad = p.m_pad, g.b_rows = q.n, g.rsteps = p.n_pad / kStep;
+    g.out[0] = q.dx, g.rows = q.m, g.rsteps = p.n_pad / kStep;
     g.vec = q.k % 4 == 0 && aligned(q.dx, 4 * size);
-    const polyq_status s = run_grad<false>(g, 1, part, st);
+    const polyq_status s = run_grad<false>(g, part, st);
     if (s != POLYQ_OK) return s;
   }
   if (dw) {
-    g.b[0] = g.b[1] = static_cast<const uint8_t*>(x);
-    g.c[0] = q.dw[0], g.c[1] = q.dw[1], g.p = q.n, g.p_pad = p.n_pad, g.b_rows = q.m, g.rsteps = p.m_pad / kStep;
+    const int m_tiles = p.m_pad / 16, c_tiles = div_up(q.k, 32);
+    const int64_t jobs = static_cast<int64_t>(m_tiles) * chunks_of(q.k), blocks = (jobs + 3) / 4;
+    mx_transpose_kernel<<<dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st>>>(static_cast<const uint8_t*>(x), xt, q.m, q.k,
+                                                                                  m_tiles, c_tiles, jobs);
+    const polyq_status s = launched();
+    if (s != POLYQ_OK) return s;
+    g.out[0] = q.dw[0], g.out[1] = q.dw[1], g.rows = q.n, g.rsteps = p.m_pad / kStep;
     g.vec = q.k % 4 == 0 && aligned(q.dw[0], 4 * size) && aligned(q.dw[1], 4 * size);
-    return run_grad<true>(g, q.mats, part, st);
+    return run_grad<true>(g, part, st);
   }
   return POLYQ_OK;
 }
@@ -394,6 +483,7 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
 size_t backward_bytes(int32_t m, int32_t n, int32_t k, int mats, int x_type, int grad_type, int dx, int dw) {
   if (!valid_shape(m, k) || !valid_shape(n, k) || !float_type(grad_type)) return 0;
   if (!float_type(x_type) && x_type != POLYQ_MX_PACKED) return 0;
+  if (m > kMaxRows || n > kMaxRows) return 0;
   return grad_plan(m, n, k, mats, x_type, grad_type, dx != 0, dw != 0).total;
 }
 
