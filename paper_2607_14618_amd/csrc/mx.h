@@ -58,10 +58,9 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t buf, uint8_t*
   __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)lds, 16, lane_offset, offset, 0, 0);
 }
 
-// 2^(byte - 127) as a float; 255 as NaN.
+// 2^(byte - 127) as the float whose exponent the conversions take; of 255, an infinity, they make NaN.
 __device__ __forceinline__ float scale_value(uint32_t byte) {
-  const uint32_t bits = byte == 0 ? 0x00400000u : byte == kNanScale ? 0x7fc00000u : byte << 23;
-  return __builtin_bit_cast(float, bits);
+  return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : byte << 23);
 }
 
 // 16 rows x 128 channels of A (rows of D) by 16 rows x 128 channels of B (columns of D), every
@@ -122,6 +121,30 @@ __device__ __forceinline__ void store4(T* p, f4 v, bool vec, int valid) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < valid) p[i] = static_cast<T>(v[i]);
+  }
+}
+// Of 16 consecutive 16-bit elements, lanes l and l + 32 hold 0 .. 3 and 4 .. 7 in `a`, 8 .. 11 and 12 .. 15 in `b`
+// (what a 32x32 product leaves in two groups of four accumulators).  The halves trade places, so that lane l
+// gets the first eight and lane l + 32 the last: one store of 16 bytes a lane in place of two of 8.
+template <class T4>
+__device__ __forceinline__ u4v pack_halves(T4 a, T4 b) {
+  const u2v u = __builtin_bit_cast(u2v, a), v = __builtin_bit_cast(u2v, b);
+  const u2v x = __builtin_bit_cast(u2v, __builtin_amdgcn_permlane32_swap(u.x, v.x, false, false));
+  const u2v y = __builtin_bit_cast(u2v, __builtin_amdgcn_permlane32_swap(u.y, v.y, false, false));
+  return u4v{x.x, y.x, x.y, y.y};
+}
+// Elements (a at `to`, b eight further on) of one row; `to` is the lane's place in `a`.  All there, rows on 16 bytes.
+template <class T>
+__device__ __forceinline__ void store_pair(T* to, f4 a, f4 b, int upper) {
+  if constexpr (sizeof(T) == 4) {
+    store4(to, a, true, 4);
+    store4(to + 8, b, true, 4);
+  } else {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    t4 p, q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = static_cast<T>(a[i]), q[i] = static_cast<T>(b[i]);
+    *reinterpret_cast<u4v*>(to + upper * 4) = pack_halves(p, q);
   }
 }
 // The same with the type known at run time.

@@ -21,29 +21,41 @@ struct Args {
   int32_t m, n, k;
   int32_t y_type, dh_type, act;
   int32_t y_vec, dh_vec;      // rows of y / dh take vector accesses of four elements
+  int32_t y_vec16;            // rows of y take 16-byte accesses
   int32_t terms, m_pad, n_pad;  // kGatedGrad: planes [terms][2][m_pad][n_pad]
   int32_t token_blocks;
 };
 
-// Four consecutive outputs (rows n0 .. n0 + 3 of the weights) of one token.  WHOLE: all of them and the token
-// are there, and rows take vector accesses.
-template <int MODE, class T, bool WHOLE>
+// dg = dh u act'(g), du = dh act(g) of four rows of the weights and one token.
+__device__ __forceinline__ void gated_grad(int act, f4 d, f4 g, f4 u, f4* dg, f4* du) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float slope;
+    const float a = activation(act, g[i], &slope);
+    (*dg)[i] = d[i] * u[i] * slope;
+    (*du)[i] = d[i] * a;
+  }
+}
+__device__ __forceinline__ f4 gated(int act, f4 g, f4 u) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) g[i] = activation(act, g[i], nullptr) * u[i];
+  return g;
+}
+
+// Four consecutive outputs (rows n0 .. n0 + 3 of the weights) of one token, which may lie behind the last.
+template <int MODE, class T>
 __device__ __forceinline__ void finish(const Args& a, int token, int n0, f4 v, f4 u) {
   if (MODE == kGatedGrad) {
-    // du = dh act(g), dg = dh u act'(g) as sums of bf16 terms; zero in the padding
-    if (!WHOLE && (token >= a.m_pad || n0 >= a.n_pad)) return;
+    // zeros in the padding
+    if (token >= a.m_pad || n0 >= a.n_pad) return;
     f4 dg = {0.f, 0.f, 0.f, 0.f}, du = {0.f, 0.f, 0.f, 0.f};
-    if (WHOLE || (token < a.m && n0 < a.n)) {
-      const int valid = WHOLE ? 4 : a.n - n0;
-      const f4 d = load4(static_cast<const T*>(a.dh) + static_cast<int64_t>(token) * a.n + n0, WHOLE || a.dh_vec, valid);
+    if (token < a.m && n0 < a.n) {
+      const int valid = a.n - n0;
+      const f4 d = load4(static_cast<const T*>(a.dh) + static_cast<int64_t>(token) * a.n + n0, a.dh_vec, valid);
+      gated_grad(a.act, d, v, u, &dg, &du);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i >= valid) break;
-        float slope;
-        const float act = activation(a.act, v[i], &slope);
-        dg[i] = d[i] * u[i] * slope;
-        du[i] = d[i] * act;
-      }
+      for (int i = 0; i < 4; ++i)
+        if (i >= valid) dg[i] = du[i] = 0.f;
     }
     const int64_t plane = static_cast<int64_t>(a.m_pad) * a.n_pad * 2;
     uint8_t* out = static_cast<uint8_t*>(a.y) + plane_at(token, n0, a.n_pad);
@@ -52,12 +64,31 @@ __device__ __forceinline__ void finish(const Args& a, int token, int n0, f4 v, f
       *reinterpret_cast<bf16x4*>(out + (2 * t + 1) * plane) = next_terms(&du);
     }
   } else {
-    if (!WHOLE && (token >= a.m || n0 >= a.n)) return;
-    if (MODE == kGated) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = activation(a.act, v[i], nullptr) * u[i];
+    if (token >= a.m || n0 >= a.n) return;
+    if (MODE == kGated) v = gated(a.act, v, u);
+    store4(static_cast<T*>(a.y) + static_cast<int64_t>(token) * a.n + n0, v, a.y_vec, a.n - n0);
+  }
+}
+
+// Two groups of four (n0 and n0 + 8; lanes l + 32 four further on), all there, rows on vectors.
+template <int MODE, class T>
+__device__ __forceinline__ void finish_pair(const Args& a, int token, int n0, int upper, f4 v, f4 u, f4 v8, f4 u8) {
+  const int64_t at = static_cast<int64_t>(token) * a.n + n0;
+  if (MODE == kGatedGrad) {
+    const T* dh = static_cast<const T*>(a.dh) + at;
+    f4 dg, du, dg8, du8;
+    gated_grad(a.act, load4(dh, true, 4), v, u, &dg, &du);
+    gated_grad(a.act, load4(dh + 8, true, 4), v8, u8, &dg8, &du8);
+    const int64_t plane = static_cast<int64_t>(a.m_pad) * a.n_pad * 2;
+    uint8_t* out = static_cast<uint8_t*>(a.y) + plane_at(token, n0 - 4 * upper, a.n_pad) + upper * 16;
+    for (int t = 0; t < a.terms; ++t) {
+      const bf16x4 g0 = next_terms(&dg), g1 = next_terms(&dg8), u0 = next_terms(&du), u1 = next_terms(&du8);
+      *reinterpret_cast<u4v*>(out + 2 * t * plane) = pack_halves(g0, g1);
+      *reinterpret_cast<u4v*>(out + (2 * t + 1) * plane) = pack_halves(u0, u1);
     }
-    store4(static_cast<T*>(a.y) + static_cast<int64_t>(token) * a.n + n0, v, WHOLE || a.y_vec, WHOLE ? 4 : a.n - n0);
+  } else {
+    if (MODE == kGated) v = gated(a.act, v, u), v8 = gated(a.act, v8, u8);
+    store_pair(static_cast<T*>(a.y) + at, v, v8, upper);
   }
 }
 
@@ -135,9 +166,9 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
       for (int w = 1; w < W; ++w) v[h] += sums[w][(h * PT + i) * TM + j][l];
     }
     const int token = (tok0 + j) * kRows + (l & 15), n0 = (tile0 + i) * kRows + (l >> 4) * 4;
-    if (a.y_type == POLYQ_MX_BF16) finish<MODE, __bf16, false>(a, token, n0, v[0], v[NM - 1]);
-    else if (a.y_type == POLYQ_MX_F16) finish<MODE, _Float16, false>(a, token, n0, v[0], v[NM - 1]);
-    else finish<MODE, float, false>(a, token, n0, v[0], v[NM - 1]);
+    if (a.y_type == POLYQ_MX_BF16) finish<MODE, __bf16>(a, token, n0, v[0], v[NM - 1]);
+    else if (a.y_type == POLYQ_MX_F16) finish<MODE, _Float16>(a, token, n0, v[0], v[NM - 1]);
+    else finish<MODE, float>(a, token, n0, v[0], v[NM - 1]);
   }
 }
 
@@ -290,23 +321,31 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
   }
 
   auto out = [&](auto t, auto whole) {
+    typedef typename decltype(t)::type T;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int token = (tbk * CT + wm * TM + j) * 32 + (lane & 31);
 #pragma unroll
       for (int i = 0; i < PT; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < 4; r += 2) {
           const int n0 = ((rb * WN + wn) * PT + i) * 32 + r * 8 + (lane >> 5) * 4;
-          const f16v &v = acc[i][j], &u = acc[NM == 2 ? PT + i : i][j];
-          finish<MODE, typename decltype(t)::type, decltype(whole)::value>(
-              a, token, n0, f4{v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]},
-              f4{u[4 * r], u[4 * r + 1], u[4 * r + 2], u[4 * r + 3]});
+          const f16v &x = acc[i][j], &y = acc[NM == 2 ? PT + i : i][j];
+          const f4 v = {x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+          const f4 u = {y[4 * r], y[4 * r + 1], y[4 * r + 2], y[4 * r + 3]};
+          const f4 v8 = {x[4 * r + 4], x[4 * r + 5], x[4 * r + 6], x[4 * r + 7]};
+          const f4 u8 = {y[4 * r + 4], y[4 * r + 5], y[4 * r + 6], y[4 * r + 7]};
+          if (decltype(whole)::value) {
+            finish_pair<MODE, T>(a, token, n0, lane >> 5, v, u, v8, u8);
+          } else {
+            finish<MODE, T>(a, token, n0, v, u);
+            finish<MODE, T>(a, token, n0 + 8, v8, u8);
+          }
         }
     }
   };
   const int type = MODE == kGatedGrad ? a.dh_type : a.y_type;
-  const bool all = (rb + 1) * (WN * PT * 32) <= a.n && (tbk + 1) * (CT * 32) <= a.m && (MODE == kGatedGrad ? a.dh_vec : a.y_vec);
+  const bool all = (rb + 1) * (WN * PT * 32) <= a.n && (tbk + 1) * (CT * 32) <= a.m && (MODE == kGatedGrad ? a.dh_vec : a.y_vec16);
   auto typed = [&](auto t) { all ? out(t, std::true_type()) : out(t, std::false_type()); };
   if (type == POLYQ_MX_BF16) typed(BF16());
   else if (type == POLYQ_MX_F16) typed(F16());
@@ -392,6 +431,7 @@ polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const
   a.y = y, a.y_type = y_type, a.act = act;
   a.m = m, a.n = n, a.k = k;
   a.y_vec = n % 4 == 0 && aligned(y, 4 * type_bytes(y_type));
+  a.y_vec16 = n * type_bytes(y_type) % 16 == 0 && aligned(y, 16);
   const polyq_status s = packed_input(x, x_type, m, k, ws, ws_bytes, &a.x, st);
   if (s != POLYQ_OK) return s;
   return act < 0 ? run<kLinear>(a, st) : run<kGated>(a, st);

@@ -43,6 +43,7 @@ struct GradArgs {
   int32_t rsteps;       // stages of one term (and matrix)
   int32_t l_blocks, s_blocks;
   int32_t type, vec;    // of the outputs; rows take vector accesses of four elements
+  int32_t vec16;        // k is a multiple of 16 and the outputs are on 16 bytes
 };
 
 // WL x WS waves, each TL x 32 l by TS x 32 s.
@@ -50,9 +51,9 @@ template <bool DW, int WL, int WS, int TL, int TS>
 __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs g) {
   constexpr int W = WL * WS, L = WL * TL * 32, S = WS * TS * 32;
   constexpr int STAGE = L * kStep * 2;
-  constexpr int DMA = STAGE / kBlockBytes / W;                    // dW: blocks a wave fetches per stage
+  constexpr int BLOCKS = STAGE / kBlockBytes / W;                 // dW: blocks a wave carries into LDS per stage
   constexpr int FRAGS = (L / kChunk) * (kStep / kRows) / W;       // dx: packed fragments a wave converts per stage
-  static_assert(DMA * W * kBlockBytes == STAGE && FRAGS * W * kChunk * kRows == L * kStep && L % kChunk == 0, "tile");
+  static_assert(BLOCKS * W * kBlockBytes == STAGE && FRAGS * W * kChunk * kRows == L * kStep && L % kChunk == 0, "tile");
   extern __shared__ uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wl = wave % WL, ws = wave / WL;
@@ -69,6 +70,14 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   const int first = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / g.splits);
   const int last = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / g.splits);
 
+  // A stage's place: plane (term and, for dx, matrix) and r step; past the end the last one's.
+  struct Place {
+    int stage, plane, r;
+  };
+  auto advance = [&](Place p) {
+    const bool more = p.stage + 1 < last, wrap = p.r + 1 == g.rsteps;
+    return Place{p.stage + 1, p.plane + (more && wrap ? 1 : 0), !more ? p.r : wrap ? 0 : p.r + 1};
+  };
   // S: fragments of the work-group's s tiles; r in tiles of 16.
   const int s_tiles = DW ? div_up(g.k, 32) : g.m_pad / 32;
   const int64_t s_tile = static_cast<int64_t>(DW ? g.m_pad : g.n_pad) / 16 * kBlockBytes;
@@ -79,43 +88,48 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
     so[i] = static_cast<uint32_t>(min(sb * (S / 32) + ws * TS + i, s_tiles - 1) - s0) * static_cast<uint32_t>(s_tile) +
             (lane & 31) * 32 + (lane >> 5) * 16;
   i4v sf[4][TS];
-  auto load_s = [&](int stage, auto which) {  // the fragments of step J of a stage (the last one again past the end)
+  auto load_s = [&](const Place& p, auto which) {  // the fragments of step J of a stage
     constexpr int J = decltype(which)::value;
-    const int st = min(stage, last - 1), r = st % g.rsteps, plane = st / g.rsteps;
-    const uint8_t* base = (DW ? g.xt : g.d + plane * g.plane) + s0 * s_tile;
+    const uint8_t* base = (DW ? g.xt : g.d + p.plane * g.plane) + s0 * s_tile;
     const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, (s_tiles - s0) * s_tile);
 #pragma unroll
     for (int i = 0; i < TS; ++i)
-      sf[J][i] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(buf, so[i], (r * 4 + J) * kBlockBytes, 0));
+      sf[J][i] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(buf, so[i], (p.r * 4 + J) * kBlockBytes, 0));
   };
 
-  // L of dW: blocks straight into LDS.
-  const int n_tiles = g.n_pad / 16;
-  auto fetch = [&](int stage, int half) {
-    const int r = stage % g.rsteps, plane = stage / g.rsteps * g.mats + mat_out;
-    const int n0 = min(lb * (L / 16), n_tiles - 1);
-    const uint8_t* base = g.d + plane * g.plane + (static_cast<int64_t>(r) * 2 * n_tiles + n0) * kBlockBytes;
+  // L of dW: whole blocks by way of registers.
+  const int n_tiles = g.n_pad / 16, n0 = min(lb * (L / 16), n_tiles - 1);
+  i4v blocks[BLOCKS];
+  auto fetch_blocks = [&](const Place& p) {
+    const uint8_t* base = g.d + (p.plane * g.mats + mat_out) * g.plane + (static_cast<int64_t>(p.r) * 2 * n_tiles + n0) * kBlockBytes;
     const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, (static_cast<int64_t>(2) * n_tiles - n0) * kBlockBytes);
 #pragma unroll
-    for (int i = 0; i < DMA; ++i) {
+    for (int i = 0; i < BLOCKS; ++i) {
       const int block = i * W + wave, rt = block / (L / 16), lt = min(lb * (L / 16) + block % (L / 16), n_tiles - 1) - n0;
-      load_to_lds(buf, lds + half * STAGE + block * kBlockBytes, lane * 16, (rt * n_tiles + lt) * kBlockBytes);
+      blocks[i] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(buf, lane * 16, (rt * n_tiles + lt) * kBlockBytes, 0));
     }
+  };
+  auto store_blocks = [&](int half) {
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i)
+      *reinterpret_cast<i4v*>(lds + half * STAGE + (i * W + wave) * kBlockBytes + lane * 16) = blocks[i];
   };
   // L of dx: packed fragments (16 r x 128 l) into registers, and from there as bf16 into LDS.
   const int chunks = chunks_of(g.k), b_tiles = tiles_of(g.n);
   i4v codes[FRAGS];
   uint32_t bytes[FRAGS];
-  auto fetch_codes = [&](int stage) {
-    const int st = min(stage, last - 1), r = st % g.rsteps, mat = st / g.rsteps % g.mats;
+  const uint8_t *w0 = g.w[0], *w1 = g.w[1];
+  int tile0 = 0;  // the first row tile of the stage in `codes`
+  auto fetch_codes = [&](const Place& p) {
+    const uint8_t* w = g.mats > 1 && (p.plane & 1) ? w1 : w0;
+    tile0 = p.r * (kStep / kRows);
 #pragma unroll
     for (int i = 0; i < FRAGS; ++i) {
-      const int f = i * W + wave, tile = r * (kStep / kRows) + f % (kStep / kRows);
+      const int f = i * W + wave, tile = min(tile0 + f % (kStep / kRows), b_tiles - 1);
       const int c = min(lb * (L / kChunk) + f / (kStep / kRows), chunks - 1);
-      const uint8_t* src = (mat ? g.w[1] : g.w[0]) + min(tile, b_tiles - 1) * tb;
+      const uint8_t* src = w + tile * tb;
       codes[i] = *reinterpret_cast<const i4v*>(src + chunk_offset(c) + lane * 16);
       bytes[i] = src[scale_offset(c) + lane * 4 + (c & 3)];
-      if (tile >= b_tiles) codes[i] = i4v{0, 0, 0, 0}, bytes[i] = 127;  // rows behind the last: zeros
     }
   };
   auto convert = [&](int half, auto which) {  // half H of each fragment's 32 channels per lane
@@ -123,19 +137,16 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
 #pragma unroll
     for (int i = 0; i < FRAGS; ++i) {
       const int f = i * W + wave, rt = f % (kStep / kRows);
-      const float s = scale_value(bytes[i]);
+      const bool there = tile0 + rt < b_tiles;  // rows behind the last tile are zeros
+      const float s = scale_value(there ? bytes[i] : 127u);
       uint32_t v[8];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        const uint32_t code = static_cast<uint32_t>(codes[i][H * 2 + w]);
+        const uint32_t code = there ? static_cast<uint32_t>(codes[i][H * 2 + w]) : 0u;
         v[w * 4 + 0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0));
         v[w * 4 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1));
         v[w * 4 + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2));
         v[w * 4 + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3));
-      }
-      if (bytes[i] == kNanScale) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0x7fc07fc0u;
       }
       const int lt = f / (kStep / kRows) * 8 + (lane >> 4) * 2 + H;
       uint8_t* dst = lds + half * STAGE + ((rt >> 1) * (L / 16) + lt) * kBlockBytes + ((rt & 1) * 16 + (lane & 15)) * 32;
@@ -179,66 +190,73 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
+  // A product occupies the matrix unit for 32 clocks; the vector work of the next stage goes in between.
+  auto mix = [&]() {
+#pragma unroll
+    for (int i = 0; i < TL * TS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(DW ? 0x200 : 0x002, DW ? 1 : 6 * FRAGS, 0);
+    }
+  };
+  Place next = {first, first / g.rsteps, first % g.rsteps};
+  auto fetch_l = [&](const Place& p) { DW ? fetch_blocks(p) : fetch_codes(p); };
   if (first < last) {
+    fetch_l(next);
+    load_s(next, I0());
+    load_s(next, I1());
+    load_s(next, I2());
+    load_s(next, I3());
     if (DW) {
-      fetch(first, 0);
+      store_blocks(0);
     } else {
-      fetch_codes(first);
       convert(0, I0());
       convert(0, I1());
-      fetch_codes(first + 1);
     }
-    load_s(first, I0());
-    load_s(first, I1());
-    load_s(first, I2());
-    load_s(first, I3());
-    __builtin_amdgcn_s_waitcnt(0x0070);
+    next = advance(next);
+    fetch_l(next);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     fence();
     read_l(0, 0, 0);
   }
-  for (int stage = first; stage < last; ++stage) {
+  for (int stage = first; stage < last; ++stage) {  // `next`: the stage after this one
     const int half = (stage - first) & 1;
     // The other half is free: every wave read the last of it before the barrier below.
-    if (DW && stage + 1 < last) fetch(stage + 1, half ^ 1);
-    fence();
     read_l(half, 1, 1);
     fence();
     multiply(I0());
     fence();
-    load_s(stage + 1, I0());
-    if (!DW) convert(half ^ 1, I0());
-    fence();
+    load_s(next, I0());
     read_l(half, 2, 0);
     fence();
     multiply(I1());
-    fence();
-    load_s(stage + 1, I1());
     if (!DW) {
-      convert(half ^ 1, I1());
-      fetch_codes(stage + 2);
+      convert(half ^ 1, I0());
+      mix();
     }
     fence();
+    load_s(next, I1());
     read_l(half, 3, 1);
     fence();
     multiply(I2());
+    if (DW) store_blocks(half ^ 1);
+    else convert(half ^ 1, I1());
+    mix();
     fence();
-    load_s(stage + 1, I2());
-    fence();
-    // The next stage's L is in LDS: dW's own loads are older than the 3 TS of S since.
-    if (DW)
-      __builtin_amdgcn_s_waitcnt(0x0070 | (3 * TS & 15) | (3 * TS >> 4 << 14));
-    else
-      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    load_s(next, I2());
+    const Place after = advance(next);
+    fetch_l(after);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the next stage's L is in LDS, this one's is read
     __builtin_amdgcn_s_barrier();
     fence();
     read_l(half ^ 1, 0, 0);
     fence();
     multiply(I3());
     fence();
-    load_s(stage + 1, I3());
+    load_s(next, I3());
+    next = after;
   }
-  const bool vec = g.splits > 1 ? g.k % 4 == 0 : g.vec;
+  const bool vec = g.splits > 1 ? g.k % 4 == 0 : g.vec, vec16 = g.splits > 1 ? g.k % 16 == 0 : g.vec16;
   auto out = [&](auto t) {
     typedef typename decltype(t)::type T;
     T* base = static_cast<T*>(g.splits > 1 ? static_cast<void*>(g.part + (static_cast<int64_t>(blockIdx.y) * (DW ? g.mats : 1) + mat_out) *
@@ -252,11 +270,18 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
         const int row = (DW ? lt : st) * 32 + (lane & 31), col = (DW ? st : lt) * 32 + (lane >> 5) * 4;
         if (row >= g.rows) continue;
         T* to = base + static_cast<int64_t>(row) * g.k + col;
+        const f16v& d = acc[i][j];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (col + r * 8 < g.k)
-            store4(to + r * 8, f4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]}, vec,
-                   g.k - col - r * 8);
+        for (int r = 0; r < 4; r += 2) {
+          const f4 v = {d[4 * r], d[4 * r + 1], d[4 * r + 2], d[4 * r + 3]};
+          const f4 v8 = {d[4 * r + 4], d[4 * r + 5], d[4 * r + 6], d[4 * r + 7]};
+          if (vec16) {  // k is a multiple of 16: all of the two groups and of both halves' is there, or none
+            if (col + r * 8 < g.k) store_pair(to + r * 8, v, v8, lane >> 5);
+          } else {
+            if (col + r * 8 < g.k) store4(to + r * 8, v, vec, g.k - col - r * 8);
+            if (col + r * 8 + 8 < g.k) store4(to + r * 8 + 8, v8, vec, g.k - col - r * 8 - 8);
+          }
+        }
       }
   };
   if (g.splits > 1 || g.type == POLYQ_MX_F32) out(F32());
@@ -287,7 +312,6 @@ __global__ __launch_bounds__(256) void mx_transpose_kernel(const uint8_t* __rest
              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
-    if (byte == kNanScale) v = u4v{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
     if (!there) v = u4v{0, 0, 0, 0};
     *reinterpret_cast<u4v*>(block + (lane & 15) * 64 + w * 16) = v;
   }
@@ -336,18 +360,26 @@ inline int64_t pad64(int64_t v) { return align_up(v, 64); }
 
 // One gradient product's tile and splits: outputs of `l` by `s`, `stages` of the reduction.
 struct Shape {
-  bool big;
+  int tile;  // of l x s: 256 x 256 by eight waves, 256 x 128 and 256 x 64 by four
   int l_blocks, s_blocks, splits;
 };
-Shape grad_shape(int l, int s, int outs, int stages) {
+Shape grad_shape(bool dw, int l, int s, int outs, int stages) {
   Shape h;
   const int64_t big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs;
-  h.big = big >= 128;
-  h.l_blocks = div_up(l, 256), h.s_blocks = div_up(s, h.big ? 256 : 64);
+  // Few tokens make short sums for dW: two work-groups a compute unit then, one's stores behind the other's
+  // products (64 tokens, 5120 x 5120: 23 us instead of 31; of 2000 tokens 285 and 294, 564 and 526 gated).
+  h.tile = big < 128 ? 64 : dw && stages <= 16 ? 128 : 256;
+  h.l_blocks = div_up(l, 256), h.s_blocks = div_up(s, h.tile);
   const int64_t groups = static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs;
-  // Split the reduction where the output's tiles leave most of the GPU idle: at least 8 stages each.
+  // Work-groups that run at once.  The reduction is split where rounds of whole tiles leave much of the GPU idle; a
+  // split costs its partial sums, about as much as 8 stages, and has at least 8.
+  const int slots = h.tile == 256 ? 256 : 512;
   h.splits = 1;
-  while (groups * h.splits * 2 <= 512 && stages / (h.splits * 2) >= 8 && h.splits < 32) h.splits *= 2;
+  int64_t best = -1;
+  for (int n = 1; n <= 32 && (n == 1 || stages / n >= 8); ++n) {
+    const int64_t rounds = (groups * n + slots - 1) / slots, cost = rounds * ((stages + n - 1) / n + (n > 1 ? 8 : 0));
+    if (best < 0 || cost < best) best = cost, h.splits = n;
+  }
   return h;
 }
 
@@ -368,10 +400,12 @@ polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
 template <bool DW>
 polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
   const int outs = DW ? g.mats : 1, stages = g.terms * g.rsteps * (DW ? 1 : g.mats);
-  const Shape h = DW ? grad_shape(g.n, g.k, outs, stages) : grad_shape(g.k, g.m, outs, stages);
+  const Shape h = DW ? grad_shape(true, g.n, g.k, outs, stages) : grad_shape(false, g.k, g.m, outs, stages);
   g.splits = h.splits, g.l_blocks = h.l_blocks, g.s_blocks = h.s_blocks;
   g.part = static_cast<float*>(part);
-  const polyq_status r = h.big ? run_tile<DW, 2, 4, 4, 2>(g, outs, st) : run_tile<DW, 4, 1, 2, 2>(g, outs, st);
+  const polyq_status r = h.tile == 256 ? run_tile<DW, 2, 4, 4, 2>(g, outs, st)
+                         : DW && h.tile == 128 ? run_tile<DW, 2, 2, 4, 2>(g, outs, st)
+                                               : run_tile<DW, 4, 1, 2, 2>(g, outs, st);
   if (r != POLYQ_OK || h.splits == 1) return r;
   const int64_t blocks = (static_cast<int64_t>(g.rows) * g.k + 1023) / 1024;
   mx_grad_sum_kernel<<<dim3(static_cast<uint32_t>(blocks), outs), dim3(256), 0, st>>>(g);
@@ -394,11 +428,11 @@ GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int gr
   p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
   p.part_bytes = 0;
   if (dx) {
-    const Shape s = grad_shape(k, m, 1, p.terms * mats * (p.n_pad / kStep));
+    const Shape s = grad_shape(false, k, m, 1, p.terms * mats * (p.n_pad / kStep));
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * m * k * 4);
   }
   if (dw) {
-    const Shape s = grad_shape(n, k, mats, p.terms * (p.m_pad / kStep));
+    const Shape s = grad_shape(true, n, k, mats, p.terms * (p.m_pad / kStep));
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * mats * n * k * 4);
   }
   p.total = p.x_bytes + p.plane_bytes + p.xt_bytes + p.part_bytes;
@@ -462,7 +496,7 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
   g.m = q.m, g.n = q.n, g.k = q.k, g.m_pad = p.m_pad, g.n_pad = p.n_pad;
   if (q.dx != nullptr) {
     g.out[0] = q.dx, g.rows = q.m, g.rsteps = p.n_pad / kStep;
-    g.vec = q.k % 4 == 0 && aligned(q.dx, 4 * size);
+    g.vec = q.k % 4 == 0 && aligned(q.dx, 4 * size), g.vec16 = q.k % 16 == 0 && aligned(q.dx, 16);
     const polyq_status s = run_grad<false>(g, part, st);
     if (s != POLYQ_OK) return s;
   }
@@ -475,6 +509,7 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
     if (s != POLYQ_OK) return s;
     g.out[0] = q.dw[0], g.out[1] = q.dw[1], g.rows = q.n, g.rsteps = p.m_pad / kStep;
     g.vec = q.k % 4 == 0 && aligned(q.dw[0], 4 * size) && aligned(q.dw[1], 4 * size);
+    g.vec16 = q.k % 16 == 0 && aligned(q.dw[0], 16) && aligned(q.dw[1], 16);
     return run_grad<true>(g, part, st);
   }
   return POLYQ_OK;

@@ -143,10 +143,6 @@ __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_kernel(const uint8_
     p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 1), v[2] = p.x, v[3] = p.y;
     p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 2), v[4] = p.x, v[5] = p.y;
     p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 3), v[6] = p.x, v[7] = p.y;
-    if (byte == kNanScale) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = s;
-    }
     T* row = out + (static_cast<int64_t>(tile) * kRows + i) * k;
     if (VEC) {
       typedef T tv __attribute__((ext_vector_type(16 / sizeof(T))));
