@@ -63,6 +63,64 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
   return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : byte << 23);
 }
 
+// ------------------------------------------------------------------ quantizing a row
+// Lane's 8 values of a row from channel k0, as fp32; zero past `k`.  VEC: the row is on 16 bytes and k a multiple
+// of a 16-byte vector.
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* row, int k0, int k, float* v) {
+  if (VEC) {
+    typedef T tv __attribute__((ext_vector_type(16 / sizeof(T))));
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 8 / N; ++h) {
+      tv r = {};
+      if (k0 + h * N < k) r = *reinterpret_cast<const tv*>(row + k0 + h * N);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[h * N + i] = static_cast<float>(r[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k0 + i < k ? static_cast<float>(row[k0 + i]) : 0.f;
+  }
+}
+// The codes of those 8 values and, the same in the block's four lanes, its scale byte.
+__device__ __forceinline__ uint32_t quantize8(const float* v, uint32_t* byte) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
+  const int e = static_cast<int>(top >> 23);
+  *byte = static_cast<uint32_t>(max(e - 2, 0));
+  const float s = scale_value(*byte);
+  uint32_t code = 0;
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], s, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], s, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], s, 2);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], s, 3);
+  if (e == 255) *byte = kNanScale, code = 0;
+  return code;
+}
+// A record of 16 rows x 512 channels in LDS.  A block of 16 rows is 272 bytes from the next, so that the 16 blocks of
+// a row fall into different banks.
+struct Record {
+  static constexpr int kPitch = kRows * 16 + 16;
+  uint8_t codes[16 * kPitch];
+  uint8_t scales[kScaleBytes];
+  // the 4 bytes of row `row` that hold lane `lane`'s 8 values
+  __device__ __forceinline__ uint32_t* at(int row, int lane) {
+    return reinterpret_cast<uint32_t*>(&codes[(lane >> 2) * kPitch + row * 16 + (lane & 3) * 4]);
+  }
+  // the scale byte of that block: chunk lane / 16, its block (lane / 4) % 4
+  __device__ __forceinline__ uint8_t* scale(int row, int lane) {
+    return &scales[(((lane >> 2) & 3) * kRows + row) * 4 + (lane >> 4)];
+  }
+  // lane `lane`'s fragment of chunk c
+  __device__ __forceinline__ u4v* fragment(int c, int lane) {
+    return reinterpret_cast<u4v*>(&codes[(c * 4 + (lane >> 4)) * kPitch + (lane & 15) * 16]);
+  }
+};
+
 // 16 rows x 128 channels of A (rows of D) by 16 rows x 128 channels of B (columns of D), every
 // 32-channel block of a row with its scale in byte `SEL` of that lane's word.  Products
 // of two 4-bit values are exact and the sums are kept in fp32.

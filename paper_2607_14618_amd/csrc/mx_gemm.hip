@@ -15,7 +15,8 @@ enum Mode { kLinear = 0, kGated = 1, kGatedGrad = 2 };
 
 struct Args {
   const uint8_t* w[2];  // packed weights (gate, up in the gated modes)
-  const uint8_t* x;     // packed activations
+  const void* x;        // packed activations, or for few tokens [m][k] of x_type
+  int32_t x_type, x_vec;  // rows of x take 16-byte accesses
   void* y;              // [m][n] of y_type; kGatedGrad: the planes
   const void* dh;       // kGatedGrad: [m][n] of dh_type
   int32_t m, n, k;
@@ -93,35 +94,42 @@ __device__ __forceinline__ void finish_pair(const Args& a, int token, int n0, in
 }
 
 // ---------------------------------------------------------------- few tokens
-// A work-group of W waves takes TN row tiles (in the gated modes TN / 2 of each matrix) by
-// TM token tiles; its waves split K and their sums meet in LDS.
-template <int MODE, int TN, int TM, int W>
+// A work-group of W waves takes TN row tiles (in the gated modes TN / 2 of each matrix) by one
+// token tile; its waves split K and their sums meet in LDS.  T: the activations' type, which
+// every wave then quantizes for its own part of K in its own LDS (one launch instead of
+// two); or `Packed`.
+struct Packed {};
+template <int MODE, class T, bool VEC, int TN, int W>
 __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
-  __shared__ f4 sums[W][TN * TM][64];
-  constexpr int NM = MODE == kLinear ? 1 : 2, PT = TN / NM;  // matrices, row tiles of each
+  constexpr bool RAW = !std::is_same<T, Packed>::value;
+  constexpr int NM = MODE == kLinear ? 1 : 2, PT = TN / NM, TM = 1;  // matrices, row tiles of each
+  union Shared {
+    f4 sums[W][TN][64];
+    Record x[RAW ? W : 1];
+  };
+  __shared__ Shared lds;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int chunks = chunks_of(a.k), row_tiles = tiles_of(a.n), token_tiles = tiles_of(a.m);
+  const int chunks = chunks_of(a.k), row_tiles = tiles_of(a.n);
   const int64_t tb = tile_bytes(a.k);
-  const int tile0 = static_cast<int>(blockIdx.x) * PT, tok0 = static_cast<int>(blockIdx.y) * TM;
+  const int tile0 = static_cast<int>(blockIdx.x) * PT;
   const int c0 = static_cast<int>(static_cast<int64_t>(chunks) * wave / W);
   const int c1 = static_cast<int>(static_cast<int64_t>(chunks) * (wave + 1) / W);
   const uint8_t* wp[TN];
-  const uint8_t* xp[TM];
 #pragma unroll
   for (int i = 0; i < TN; ++i) wp[i] = a.w[i / PT] + min(tile0 + i % PT, row_tiles - 1) * tb;
+  f4 acc[TN];
 #pragma unroll
-  for (int j = 0; j < TM; ++j) xp[j] = a.x + min(tok0 + j, token_tiles - 1) * tb;
-  f4 acc[TN][TM];
-#pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < TN; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
+  Record& rec = lds.x[RAW ? wave : 0];
+  if (RAW) {  // tokens behind the last: code 0, scale 1
+    for (int i = lane; i < static_cast<int>(sizeof(rec.codes) / 16); i += 64) reinterpret_cast<u4v*>(rec.codes)[i] = u4v{0, 0, 0, 0};
+    reinterpret_cast<uint32_t*>(rec.scales)[lane] = 0x7f7f7f7fu;
+  }
 
-  constexpr int U = TN * TM <= 4 ? 4 : 2;
   auto step = [&](int c, auto count) {
     constexpr int N = decltype(count)::value;
-    i4v ca[N][TN], cb[N][TM];
-    uint32_t sa[N][TN], sb[N][TM];
+    i4v ca[N][TN], cb[N];
+    uint32_t sa[N][TN], sb[N];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int64_t at = chunk_offset(c + u) + lane * 16, sat = scale_offset(c + u) + lane * 4;
@@ -130,10 +138,27 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
         ca[u][i] = *reinterpret_cast<const i4v*>(wp[i] + at);
         sa[u][i] = *reinterpret_cast<const uint32_t*>(wp[i] + sat);
       }
+      if constexpr (!RAW) {
+        cb[u] = *reinterpret_cast<const i4v*>(static_cast<const uint8_t*>(a.x) + at);
+        sb[u] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.x) + sat);
+      }
+    }
+    if constexpr (RAW) {  // channels 128 c .. of all tokens, as a record of which N chunks are read
+      const int k0 = c * kChunk + lane * 8;
+      for (int t = 0; t < a.m; ++t) {
+        float v[8];
+        load8<T, VEC>(static_cast<const T*>(a.x) + static_cast<int64_t>(t) * a.k, k0, a.k, v);
+        uint32_t byte;
+        const uint32_t code = quantize8(v, &byte);
+        *rec.at(t, lane) = code;
+        if ((lane & 3) == 0) *rec.scale(t, lane) = static_cast<uint8_t>(byte);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const uint32_t word = reinterpret_cast<const uint32_t*>(rec.scales)[lane];
 #pragma unroll
-      for (int j = 0; j < TM; ++j) {
-        cb[u][j] = *reinterpret_cast<const i4v*>(xp[j] + at);
-        sb[u][j] = *reinterpret_cast<const uint32_t*>(xp[j] + sat);
+      for (int u = 0; u < N; ++u) {
+        cb[u] = __builtin_bit_cast(i4v, *rec.fragment(u, lane));
+        sb[u] = word >> (8 * u) << (8 * ((c + u) & 3));
       }
     }
 #pragma unroll
@@ -141,31 +166,30 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
       const int sh = 8 * ((c + u) & 3);
 #pragma unroll
       for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j)
-          acc[i][j] = mfma_mx<0, 0>(ca[u][i], cb[u][j], acc[i][j], static_cast<int>(sa[u][i] >> sh),
-                                    static_cast<int>(sb[u][j] >> sh));
+        acc[i] = mfma_mx<0, 0>(ca[u][i], cb[u], acc[i], static_cast<int>(sa[u][i] >> sh), static_cast<int>(sb[u] >> sh));
     }
   };
+  constexpr int U = 4;
   int c = c0;
   for (; c + U <= c1; c += U) step(c, std::integral_constant<int, U>());
-  for (; c < c1; ++c) step(c, std::integral_constant<int, 1>());
+  if (c1 - c == 3) step(c, std::integral_constant<int, 3>());
+  else if (c1 - c == 2) step(c, std::integral_constant<int, 2>());
+  else if (c1 - c == 1) step(c, std::integral_constant<int, 1>());
 
+  if (RAW) __syncthreads();  // the sums take the records' place
 #pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int j = 0; j < TM; ++j) sums[wave][i * TM + j][lane] = acc[i][j];
+  for (int i = 0; i < TN; ++i) lds.sums[wave][i][lane] = acc[i];
   __syncthreads();
-  for (int item = threadIdx.x; item < PT * TM * 64; item += 64 * W) {
-    const int l = item & 63, ij = item >> 6, i = ij / TM, j = ij % TM;
+  for (int item = threadIdx.x; item < PT * 64; item += 64 * W) {
+    const int l = item & 63, i = item >> 6;
     f4 v[NM];
 #pragma unroll
     for (int h = 0; h < NM; ++h) {
-      v[h] = sums[0][(h * PT + i) * TM + j][l];
+      v[h] = lds.sums[0][h * PT + i][l];
 #pragma unroll
-      for (int w = 1; w < W; ++w) v[h] += sums[w][(h * PT + i) * TM + j][l];
+      for (int w = 1; w < W; ++w) v[h] += lds.sums[w][h * PT + i][l];
     }
-    const int token = (tok0 + j) * kRows + (l & 15), n0 = (tile0 + i) * kRows + (l >> 4) * 4;
+    const int token = l & 15, n0 = (tile0 + i) * kRows + (l >> 4) * 4;
     if (a.y_type == POLYQ_MX_BF16) finish<MODE, __bf16>(a, token, n0, v[0], v[NM - 1]);
     else if (a.y_type == POLYQ_MX_F16) finish<MODE, _Float16>(a, token, n0, v[0], v[NM - 1]);
     else finish<MODE, float>(a, token, n0, v[0], v[NM - 1]);
@@ -202,7 +226,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
   const int row0 = min(rb * WN * PT * 2, row_tiles - 1), tok0 = min(tbk * CT * 2, token_tiles - 1);
   const __amdgpu_buffer_rsrc_t wbuf0 = make_rsrc(a.w[0] + row0 * tb, (row_tiles - row0) * tb);
   const __amdgpu_buffer_rsrc_t wbuf1 = make_rsrc(a.w[NM - 1] + row0 * tb, (row_tiles - row0) * tb);
-  const __amdgpu_buffer_rsrc_t xbuf = make_rsrc(a.x + tok0 * tb, (token_tiles - tok0) * tb);
+  const __amdgpu_buffer_rsrc_t xbuf = make_rsrc(static_cast<const uint8_t*>(a.x) + tok0 * tb, (token_tiles - tok0) * tb);
   const uint32_t tb32 = static_cast<uint32_t>(tb);
   uint32_t wo[PT], xo[TM];
 #pragma unroll
@@ -355,12 +379,15 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
 // ---------------------------------------------------------------- launches
 polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
 
-template <int MODE, int TN, int TM, int W>
+template <int MODE, class T, bool VEC>
 polyq_status run_stream(const Args& a, hipStream_t st) {
-  const int pt = TN / (MODE == kLinear ? 1 : 2);
-  const dim3 grid(div_up(tiles_of(a.n), pt), div_up(tiles_of(a.m), TM));
-  mx_stream_kernel<MODE, TN, TM, W><<<grid, dim3(64 * W), 0, st>>>(a);
+  constexpr int TN = MODE == kLinear ? 1 : 2, W = 8;
+  mx_stream_kernel<MODE, T, VEC, TN, W><<<dim3(tiles_of(a.n)), dim3(64 * W), 0, st>>>(a);
   return launched();
+}
+template <int MODE, class T>
+polyq_status run_raw(const Args& a, hipStream_t st) {
+  return a.x_vec ? run_stream<MODE, T, true>(a, st) : run_stream<MODE, T, false>(a, st);
 }
 
 template <int MODE, int WN, int WM, int TN, int TM>
@@ -381,7 +408,12 @@ polyq_status run_gemm(Args a, hipStream_t st) {
 
 template <int MODE>
 polyq_status run(const Args& a, hipStream_t st) {
-  if (MODE != kGatedGrad && a.m <= 16) return run_stream<MODE, MODE == kLinear ? 1 : 2, 1, 8>(a, st);
+  if constexpr (MODE != kGatedGrad) {
+    if (a.x_type == POLYQ_MX_F32) return run_raw<MODE, float>(a, st);
+    if (a.x_type == POLYQ_MX_F16) return run_raw<MODE, _Float16>(a, st);
+    if (a.x_type == POLYQ_MX_BF16) return run_raw<MODE, __bf16>(a, st);
+    if (a.m <= 16) return run_stream<MODE, Packed, true>(a, st);
+  }
   const int64_t tiles = static_cast<int64_t>(tiles_of(a.n)) * (MODE == kLinear ? 1 : 2) * tiles_of(a.m);
   if (tiles >= 128 * 128) return run_gemm<MODE, 4, 1, 2, 4>(a, st);
   return run_gemm<MODE, 4, 1, 2, 2>(a, st);
@@ -394,7 +426,7 @@ polyq_status launch_gated_grad(const void* gate, const void* up, const void* x, 
                                hipStream_t st) {
   Args a{};
   a.w[0] = static_cast<const uint8_t*>(gate), a.w[1] = static_cast<const uint8_t*>(up);
-  a.x = static_cast<const uint8_t*>(x);
+  a.x = x, a.x_type = POLYQ_MX_PACKED;
   a.y = planes, a.dh = dh, a.dh_type = dh_type;
   a.m = m, a.n = n, a.k = k, a.act = act;
   a.terms = terms, a.m_pad = m_pad, a.n_pad = n_pad;
@@ -404,16 +436,8 @@ polyq_status launch_gated_grad(const void* gate, const void* up, const void* x, 
 
 namespace {
 
-// The activations' packed form: as given, or quantized into the workspace.
-polyq_status packed_input(const void* x, int x_type, int32_t m, int32_t k, void* ws, size_t ws_bytes, const uint8_t** out,
-                          hipStream_t st) {
-  if (x_type == POLYQ_MX_PACKED) {
-    *out = static_cast<const uint8_t*>(x);
-    return POLYQ_OK;
-  }
-  *out = static_cast<const uint8_t*>(ws);
-  return launch_quantize(x, x_type, m, k, ws, st);
-}
+// Up to this many tokens every work-group quantizes the activations itself.
+constexpr int kRawTokens = 4;
 
 polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const void* w1, int32_t n, int32_t k, int act,
                      void* y, int y_type, void* ws, size_t ws_bytes, hipStream_t st) {
@@ -432,8 +456,13 @@ polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const
   a.m = m, a.n = n, a.k = k;
   a.y_vec = n % 4 == 0 && aligned(y, 4 * type_bytes(y_type));
   a.y_vec16 = n * type_bytes(y_type) % 16 == 0 && aligned(y, 16);
-  const polyq_status s = packed_input(x, x_type, m, k, ws, ws_bytes, &a.x, st);
-  if (s != POLYQ_OK) return s;
+  a.x = x, a.x_type = x_type;
+  a.x_vec = x_type != POLYQ_MX_PACKED && aligned(x, 16) && static_cast<int64_t>(k) * type_bytes(x_type) % 16 == 0;
+  if (need > 0) {
+    const polyq_status s = launch_quantize(x, x_type, m, k, ws, st);
+    if (s != POLYQ_OK) return s;
+    a.x = ws, a.x_type = POLYQ_MX_PACKED;
+  }
   return act < 0 ? run<kLinear>(a, st) : run<kGated>(a, st);
 }
 
@@ -444,7 +473,7 @@ polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const
 using namespace polyq;
 
 extern "C" size_t polyq_mx_workspace_bytes(int32_t m, int32_t k, int32_t x_type) {
-  return mx::float_type(x_type) ? polyq_mx_bytes(m, k) : 0;
+  return mx::float_type(x_type) && m > mx::kRawTokens ? polyq_mx_bytes(m, k) : 0;
 }
 
 extern "C" polyq_status polyq_mx_linear(const void* x, int32_t x_type, int32_t m, const void* w, int32_t n, int32_t k,

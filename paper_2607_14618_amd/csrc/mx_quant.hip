@@ -8,11 +8,10 @@
 // division by a power of two is exact, so nothing rounds but the value itself.  A block
 // that holds an infinity or a NaN gets the NaN scale: all of it is NaN.
 //
-// What bounds it: memory; 2 to 4 bytes are read and 17/32 written per value.  A wave
-// takes one record, 16 rows x 512 values: row by row the 64 lanes read 8 values each (1
-// or 2 KiB in a row), form the block's maximum over 4 lanes and convert; the codes meet
-// in LDS, from where they leave as whole 1 KiB fragments.  A block in LDS is 272 bytes
-// apart, so that the 16 blocks of a row fall into different banks.
+// What bounds it: memory; 2 to 4 bytes are read and 17/32 written per value.  A work-group
+// takes one record, 16 rows x 512 values, a wave four of its rows: the 64 lanes read 8
+// values each of a row (1 or 2 KiB in a row), form the block's maximum over 4 lanes and
+// convert; the codes meet in LDS, from where they leave as whole 1 KiB fragments.
 #include <hip/hip_runtime.h>
 
 #include "mx.h"
@@ -21,121 +20,55 @@ namespace polyq {
 namespace mx {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kBlockPitch = kRows * 16 + 16;  // bytes of a block of 16 rows in LDS
-
-struct Record {  // one wave's LDS
-  uint8_t codes[16 * kBlockPitch];
-  uint32_t scales[64];
-};
-
-// LDS address of the 4 bytes of row `row` that lane `lane`'s 8 values occupy.
-__device__ __forceinline__ int code_slot(int row, int lane) { return (lane >> 2) * kBlockPitch + row * 16 + (lane & 3) * 4; }
-
-// Lane's 8 values of a row (k0 = its first channel), as fp32; zero past `k`.
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, int k0, int k, float* v) {
-  if (VEC) {  // row is 16-byte aligned and k a multiple of the vector
-    typedef T tv __attribute__((ext_vector_type(16 / sizeof(T))));
-    constexpr int N = 16 / sizeof(T);
-#pragma unroll
-    for (int h = 0; h < 8 / N; ++h) {
-      tv r = {};
-      if (k0 + h * N < k) r = *reinterpret_cast<const tv*>(row + k0 + h * N);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[h * N + i] = static_cast<float>(r[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k0 + i < k ? static_cast<float>(row[k0 + i]) : 0.f;
-  }
-}
+constexpr int kWaves = 4, kWaveRows = kRows / kWaves;
 
 template <class T, bool VEC>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_kernel(const T* __restrict__ x, uint8_t* __restrict__ packed,
-                                                                  int rows, int k, int records, int64_t jobs) {
-  __shared__ Record lds[kWaves];
+                                                                  int rows, int k, int records) {
+  __shared__ Record r;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
-  if (job >= jobs) return;  // waves are independent: no barrier follows
-  const int tile = static_cast<int>(job / records), rec = static_cast<int>(job % records);
-  Record& r = lds[wave];
-  const int k0 = rec * kRec + lane * 8;
-  const int valid = min(kRows, rows - tile * kRows);
-  constexpr int U = sizeof(T) == 4 ? 4 : 8;  // rows in flight
-  uint8_t* sc = reinterpret_cast<uint8_t*>(r.scales);
-  for (int i0 = 0; i0 < kRows; i0 += U) {
-    float v[U][8];
+  const int tile = static_cast<int>(blockIdx.x / records), rec = static_cast<int>(blockIdx.x % records);
+  const int k0 = rec * kRec + lane * 8, row0 = tile * kRows + wave * kWaveRows;
+  float v[kWaveRows][8];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+  for (int u = 0; u < kWaveRows; ++u) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
-      if (i0 + u < valid) load8<T, VEC>(x + (static_cast<int64_t>(tile) * kRows + i0 + u) * k, k0, k, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, v[u][i]) & 0x7fffffffu);
-      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
-      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
-      const int e = static_cast<int>(top >> 23);
-      uint32_t byte = static_cast<uint32_t>(max(e - 2, 0));
-      const float s = scale_value(byte);
-      uint32_t code = 0;
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[u][0], v[u][1], s, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[u][2], v[u][3], s, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[u][4], v[u][5], s, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[u][6], v[u][7], s, 3);
-      if (e == 255) byte = kNanScale, code = 0;
-      // rows behind the last and channels behind k: code 0 with scale 1
-      const bool none = i0 + u >= valid || rec * kRec + (lane >> 2) * kBlock >= k;
-      *reinterpret_cast<uint32_t*>(&r.codes[code_slot(i0 + u, lane)]) = none ? 0u : code;
-      if ((lane & 3) == 0) {  // block lane / 4 of the record: chunk lane / 16, its block (lane / 4) % 4
-        const int q = (lane >> 2) & 3;
-        sc[(q * kRows + i0 + u) * 4 + (lane >> 4)] = static_cast<uint8_t>(none ? 127u : byte);
-      }
-    }
+    for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+    if (row0 + u < rows) load8<T, VEC>(x + static_cast<int64_t>(row0 + u) * k, k0, k, v[u]);
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int u = 0; u < kWaveRows; ++u) {
+    uint32_t byte;
+    const uint32_t code = quantize8(v[u], &byte);
+    // rows behind the last and blocks behind k: code 0 with scale 1
+    const bool none = row0 + u >= rows || rec * kRec + (lane >> 2) * kBlock >= k;
+    *r.at(wave * kWaveRows + u, lane) = none ? 0u : code;
+    if ((lane & 3) == 0) *r.scale(wave * kWaveRows + u, lane) = static_cast<uint8_t>(none ? 127u : byte);
+  }
+  __syncthreads();
   uint8_t* out = packed + tile * tile_bytes(k) + static_cast<int64_t>(rec) * kRecBytes;
-  reinterpret_cast<uint32_t*>(out)[lane] = r.scales[lane];
-  const int chunks = min(4, chunks_of(k) - rec * 4);
-  for (int c = 0; c < chunks; ++c) {
-    const u4v w = *reinterpret_cast<const u4v*>(&r.codes[(c * 4 + (lane >> 4)) * kBlockPitch + (lane & 15) * 16]);
-    *reinterpret_cast<u4v*>(out + kScaleBytes + c * kChunkBytes + lane * 16) = w;
-  }
+  if (wave < chunks_of(k) - rec * 4) *reinterpret_cast<u4v*>(out + kScaleBytes + wave * kChunkBytes + lane * 16) = *r.fragment(wave, lane);
+  if (wave == 0) reinterpret_cast<uint32_t*>(out)[lane] = reinterpret_cast<const uint32_t*>(r.scales)[lane];
 }
 
 template <class T, bool VEC>
 __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_kernel(const uint8_t* __restrict__ packed, T* __restrict__ out,
-                                                                    int rows, int k, int records, int64_t jobs) {
-  __shared__ Record lds[kWaves];
+                                                                    int rows, int k, int records) {
+  __shared__ Record r;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
-  if (job >= jobs) return;
-  const int tile = static_cast<int>(job / records), rec = static_cast<int>(job % records);
-  Record& r = lds[wave];
+  const int tile = static_cast<int>(blockIdx.x / records), rec = static_cast<int>(blockIdx.x % records);
   const uint8_t* in = packed + tile * tile_bytes(k) + static_cast<int64_t>(rec) * kRecBytes;
-  const int chunks = min(4, chunks_of(k) - rec * 4);
-  r.scales[lane] = reinterpret_cast<const uint32_t*>(in)[lane];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (c < chunks) {
-      const u4v w = *reinterpret_cast<const u4v*>(in + kScaleBytes + c * kChunkBytes + lane * 16);
-      *reinterpret_cast<u4v*>(&r.codes[(c * 4 + (lane >> 4)) * kBlockPitch + (lane & 15) * 16]) = w;
-    }
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  const uint8_t* sc = reinterpret_cast<const uint8_t*>(r.scales);
-  const int k0 = rec * kRec + lane * 8, valid = min(kRows, rows - tile * kRows);
+  if (wave < chunks_of(k) - rec * 4) *r.fragment(wave, lane) = *reinterpret_cast<const u4v*>(in + kScaleBytes + wave * kChunkBytes + lane * 16);
+  if (wave == 0) reinterpret_cast<uint32_t*>(r.scales)[lane] = reinterpret_cast<const uint32_t*>(in)[lane];
+  __syncthreads();
+  const int k0 = rec * kRec + lane * 8;
   if (k0 >= k) return;  // also the lanes of chunks that are not there
-  const int q = (lane >> 2) & 3;
-#pragma unroll 4
-  for (int i = 0; i < valid; ++i) {
-    const uint32_t code = *reinterpret_cast<const uint32_t*>(&r.codes[code_slot(i, lane)]);
-    const uint32_t byte = sc[(q * kRows + i) * 4 + (lane >> 4)];
-    const float s = scale_value(byte);
+#pragma unroll
+  for (int u = 0; u < kWaveRows; ++u) {
+    const int i = wave * kWaveRows + u;
+    if (tile * kRows + i >= rows) return;
+    const uint32_t code = *r.at(i, lane);
+    const float s = scale_value(*r.scale(i, lane));
     float v[8];
     typedef float f2 __attribute__((ext_vector_type(2)));
     f2 p;
@@ -230,16 +163,16 @@ polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : PO
 
 polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, void* packed, hipStream_t st) {
   const int records = records_of(k);
-  const int64_t jobs = static_cast<int64_t>(tiles_of(rows)) * records, groups = (jobs + kWaves - 1) / kWaves;
+  const int64_t groups = static_cast<int64_t>(tiles_of(rows)) * records;
   if (check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
   const bool vec = aligned(x, 16) && static_cast<int64_t>(k) * type_bytes(type) % 16 == 0;
   uint8_t* out = static_cast<uint8_t*>(packed);
   const dim3 grid(static_cast<uint32_t>(groups)), block(64 * kWaves);
 #define POLYQ_MX_QUANTIZE(T)                                                                                        \
   if (vec)                                                                                                          \
-    mx_quantize_kernel<T, true><<<grid, block, 0, st>>>(static_cast<const T*>(x), out, rows, k, records, jobs);      \
+    mx_quantize_kernel<T, true><<<grid, block, 0, st>>>(static_cast<const T*>(x), out, rows, k, records);      \
   else                                                                                                              \
-    mx_quantize_kernel<T, false><<<grid, block, 0, st>>>(static_cast<const T*>(x), out, rows, k, records, jobs)
+    mx_quantize_kernel<T, false><<<grid, block, 0, st>>>(static_cast<const T*>(x), out, rows, k, records)
   if (type == POLYQ_MX_F32) {
     POLYQ_MX_QUANTIZE(float);
   } else if (type == POLYQ_MX_F16) {
@@ -275,7 +208,7 @@ extern "C" polyq_status polyq_mx_dequantize(const void* packed, int32_t rows, in
   if (!mx::valid_shape(rows, k)) return POLYQ_ERR_SHAPE;
   if (!mx::aligned(packed, 256) || !mx::aligned(out, mx::type_bytes(type))) return POLYQ_ERR_ARG;
   const int records = mx::records_of(k);
-  const int64_t jobs = static_cast<int64_t>(mx::tiles_of(rows)) * records, groups = (jobs + mx::kWaves - 1) / mx::kWaves;
+  const int64_t groups = static_cast<int64_t>(mx::tiles_of(rows)) * records;
   if (mx::check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
   const bool vec = mx::aligned(out, 16) && static_cast<int64_t>(k) * mx::type_bytes(type) % 16 == 0;
   const uint8_t* in = static_cast<const uint8_t*>(packed);
@@ -283,9 +216,9 @@ extern "C" polyq_status polyq_mx_dequantize(const void* packed, int32_t rows, in
   hipStream_t st = static_cast<hipStream_t>(stream);
 #define POLYQ_MX_DEQUANTIZE(T)                                                                                      \
   if (vec)                                                                                                          \
-    mx::mx_dequantize_kernel<T, true><<<grid, block, 0, st>>>(in, static_cast<T*>(out), rows, k, records, jobs);     \
+    mx::mx_dequantize_kernel<T, true><<<grid, block, 0, st>>>(in, static_cast<T*>(out), rows, k, records);     \
   else                                                                                                              \
-    mx::mx_dequantize_kernel<T, false><<<grid, block, 0, st>>>(in, static_cast<T*>(out), rows, k, records, jobs)
+    mx::mx_dequantize_kernel<T, false><<<grid, block, 0, st>>>(in, static_cast<T*>(out), rows, k, records)
   if (type == POLYQ_MX_F32) {
     POLYQ_MX_DEQUANTIZE(float);
   } else if (type == POLYQ_MX_F16) {

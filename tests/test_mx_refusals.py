@@ -49,7 +49,7 @@ def test_pack_refusals(codes, scales, rows, k, packed, want):
     assert call("polyq_mx_unpack", packed, rows, k, codes, scales, None) == want
 
 
-GOOD = dict(x=P, xt=2, m=2, w=P, n=16, k=64, y=P, yt=2, ws=P, wsb=BIG)
+GOOD = dict(x=P, xt=2, m=20, w=P, n=16, k=64, y=P, yt=2, ws=P, wsb=BIG)
 BAD = [(dict(x=NULL), ARG), (dict(w=NULL), ARG), (dict(y=NULL), ARG), (dict(xt=4), ARG), (dict(yt=3), ARG),
        (dict(m=0), ARG), (dict(m=-1), ARG), (dict(n=0), SHAPE), (dict(k=0), SHAPE), (dict(n=(1 << 24) + 1), SHAPE),
        (dict(k=(1 << 20) + 1), SHAPE), (dict(w=ODD), ARG), (dict(x=ODD), ARG), (dict(y=ODD), ARG),
