@@ -3,6 +3,7 @@
 // g, u once more in its backward pass, where dg and du leave instead of h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "mx.h"
@@ -102,7 +103,7 @@ struct Packed {};
 template <int MODE, class T, bool VEC, int TN, int W>
 __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
   constexpr bool RAW = !std::is_same<T, Packed>::value;
-  constexpr int NM = MODE == kLinear ? 1 : 2, PT = TN / NM, TM = 1;  // matrices, row tiles of each
+  constexpr int NM = MODE == kLinear ? 1 : 2, PT = TN / NM;  // matrices, row tiles of each
   union Shared {
     f4 sums[W][TN][64];
     Record x[RAW ? W : 1];
@@ -196,13 +197,106 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
   }
 }
 
+// ---------------------------------------------------------------- some tokens
+// A work-group of W waves takes 32 rows (of each matrix) by TM x 32 tokens, its waves split K, and
+// their sums meet in LDS: many work-groups where the outputs are few.  Both operands
+// come straight from memory, the tokens from L2.
+template <int MODE, int TM, int W>
+__global__ __launch_bounds__(64 * W, 2) void mx_split_kernel(const Args a) {
+  constexpr int NM = MODE == kLinear ? 1 : 2;
+  extern __shared__ f4 sums[];  // [W][NM][TM][4][64]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int second = (lane >> 4) & 1, at16 = (lane >> 5) * 256 + (lane & 15) * 16, at4 = at16 >> 2;
+  const int rb = static_cast<int>(blockIdx.x) / a.token_blocks, tbk = static_cast<int>(blockIdx.x) % a.token_blocks;
+  const int chunks = chunks_of(a.k), row_tiles = tiles_of(a.n), token_tiles = tiles_of(a.m);
+  const int64_t tb = tile_bytes(a.k);
+  const int c0 = static_cast<int>(static_cast<int64_t>(chunks) * wave / W);
+  const int c1 = static_cast<int>(static_cast<int64_t>(chunks) * (wave + 1) / W);
+  const uint8_t *wp[NM], *xp[TM];
+#pragma unroll
+  for (int i = 0; i < NM; ++i) wp[i] = a.w[i] + min(rb * 2 + second, row_tiles - 1) * tb;
+#pragma unroll
+  for (int j = 0; j < TM; ++j)
+    xp[j] = static_cast<const uint8_t*>(a.x) + min((tbk * TM + j) * 2 + second, token_tiles - 1) * tb;
+  f16v acc[NM][TM];
+#pragma unroll
+  for (int i = 0; i < NM; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  auto step = [&](int c, auto count) {
+    constexpr int N = decltype(count)::value;
+    i4v ca[N][NM][2], cb[N][TM][2];
+    uint32_t sa[N][NM][2], sb[N][TM][2];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int64_t at = chunk_offset(c + u) + at16, sat = scale_offset(c + u) + at4;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < NM; ++i) {
+          ca[u][i][h] = *reinterpret_cast<const i4v*>(wp[i] + at + h * 512);
+          sa[u][i][h] = *reinterpret_cast<const uint32_t*>(wp[i] + sat + h * 128);
+        }
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+          cb[u][j][h] = *reinterpret_cast<const i4v*>(xp[j] + at + h * 512);
+          sb[u][j][h] = *reinterpret_cast<const uint32_t*>(xp[j] + sat + h * 128);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int sh = 8 * ((c + u) & 3);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+          for (int i = 0; i < NM; ++i)
+            acc[i][j] = mfma_mx32<0, 0>(ca[u][i][h], cb[u][j][h], acc[i][j], static_cast<int>(sa[u][i][h] >> sh),
+                                        static_cast<int>(sb[u][j][h] >> sh));
+    }
+  };
+  int c = c0;
+  for (; c + 2 <= c1; c += 2) step(c, std::integral_constant<int, 2>());
+  if (c < c1) step(c, std::integral_constant<int, 1>());
+#pragma unroll
+  for (int i = 0; i < NM; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        sums[(((wave * NM + i) * TM + j) * 4 + r) * 64 + lane] =
+            f4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
+  __syncthreads();
+  auto out = [&](auto t) {
+    for (int item = threadIdx.x; item < TM * 256; item += 64 * W) {
+      f4 v[NM];
+#pragma unroll
+      for (int i = 0; i < NM; ++i) {
+        v[i] = sums[i * TM * 256 + item];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v[i] += sums[(w * NM + i) * TM * 256 + item];
+      }
+      const int l = item & 63, r = (item >> 6) & 3, j = item >> 8;
+      finish<MODE, typename decltype(t)::type>(a, (tbk * TM + j) * 32 + (l & 31), rb * 32 + r * 8 + (l >> 5) * 4, v[0], v[NM - 1]);
+    }
+  };
+  const int type = MODE == kGatedGrad ? a.dh_type : a.y_type;
+  if (type == POLYQ_MX_BF16) out(BF16());
+  else if (type == POLYQ_MX_F16) out(F16());
+  else out(F32());
+}
+
 // ---------------------------------------------------------------- many tokens
 // WN x WM waves, each TN x 32 rows (the gated modes: TN / 2 x 32 of each matrix) by TM x 32
 // tokens.  K is walked a record (4 chunks) at a time.  The tokens' fragments go from
 // memory straight into one half of a ring in LDS while the other half is multiplied; the
 // weights' fragments are what their wave alone multiplies and go into its registers,
 // two chunks ahead.
-template <int MODE, int WN, int WM, int TN, int TM>
+template <int MODE, int WN, int WM, int TN, int TM, int AHEAD>
 __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) {
   constexpr int W = WN * WM, CT = WM * TM;
   constexpr int NM = MODE == kLinear ? 1 : 2, PT = TN / NM;
@@ -265,7 +359,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
       for (int j = 0; j < TM; ++j) sb[j][h] = nb[j][h];
     }
   };
-  i4v ca[2][TN][2], cb[2][TM];
+  i4v ca[AHEAD][TN][2], cb[2][TM];
   auto weights = [&](int c, int to) {
     const uint32_t at = chunk_at(c);
 #pragma unroll
@@ -292,7 +386,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
 #pragma unroll
     for (int j = 0; j < TM; ++j)
 #pragma unroll
-      for (int i = 0; i < TN; ++i) acc[i][j] = mfma_mx32<C, C>(ca[C & 1][i][H], cb[H][j], acc[i][j], sa[i][H], sb[j][H]);
+      for (int i = 0; i < TN; ++i) acc[i][j] = mfma_mx32<C, C>(ca[C % AHEAD][i][H], cb[H][j], acc[i][j], sa[i][H], sb[j][H]);
   };
   // One chunk: two halves, the second's and then the next chunk's token fragments read ahead of the products.
   auto chunk = [&](int rec, int ring, auto which) {
@@ -306,7 +400,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
     } else {
       // The next record's tokens have arrived: their loads are older than the 2 TN latest, and than the last
       // chunk's weights that the products above have waited for.  All waves are past their reads of this record.
-      __builtin_amdgcn_s_waitcnt(0x0070 | (2 * TN));  // vmcnt(2 TN) lgkmcnt(0)
+      constexpr int SINCE = 2 * TN * (AHEAD - 1);
+      __builtin_amdgcn_s_waitcnt(0x0070 | (SINCE & 15) | (SINCE >> 4 << 14));  // vmcnt(SINCE) lgkmcnt(0)
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       tokens(ring ^ 1, 0, 0);
@@ -314,14 +409,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
     __builtin_amdgcn_sched_barrier(0);
     multiply(which, std::integral_constant<int, 1>());
     __builtin_amdgcn_sched_barrier(0);
-    weights(rec * 4 + C + 2, C & 1);
+    weights(rec * 4 + C + AHEAD, C % AHEAD);
     __builtin_amdgcn_sched_barrier(0);
   };
   fetch(0, 0);
   scales(0);
   asm volatile("" ::: "memory");
-  weights(0, 0);
-  weights(1, 1);
+#pragma unroll
+  for (int c = 0; c < AHEAD; ++c) weights(c, c);
   __builtin_amdgcn_s_waitcnt(0x0070);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -390,20 +485,65 @@ polyq_status run_raw(const Args& a, hipStream_t st) {
   return a.x_vec ? run_stream<MODE, T, true>(a, st) : run_stream<MODE, T, false>(a, st);
 }
 
-template <int MODE, int WN, int WM, int TN, int TM>
+template <int MODE, int TM, int W>
+polyq_status run_split(Args a, hipStream_t st) {
+  a.token_blocks = div_up(MODE == kGatedGrad ? a.m_pad : a.m, TM * 32);
+  const int64_t groups = static_cast<int64_t>(div_up(MODE == kGatedGrad ? a.n_pad : a.n, 32)) * a.token_blocks;
+  if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
+  const size_t lds = static_cast<size_t>(W) * (MODE == kLinear ? 1 : 2) * TM * 4096;
+  mx_split_kernel<MODE, TM, W><<<dim3(static_cast<uint32_t>(groups)), dim3(64 * W), lds, st>>>(a);
+  return launched();
+}
+
+template <int MODE, int WN, int WM, int TN, int TM, int AHEAD>
 polyq_status run_gemm(Args a, hipStream_t st) {
   const int pt = WN * TN / (MODE == kLinear ? 1 : 2);
   a.token_blocks = div_up(MODE == kGatedGrad ? a.m_pad : a.m, WM * TM * 32);
   const int64_t groups = static_cast<int64_t>(div_up(MODE == kGatedGrad ? a.n_pad : a.n, pt * 32)) * a.token_blocks;
   if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
   const size_t lds = 16 * static_cast<size_t>(WM * TM) * kChunkBytes;
-  const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM>;
+  const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM, AHEAD>;
   if (lds > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(lds)) != hipSuccess)
     return POLYQ_ERR_DEVICE;
   kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(64 * WN * WM), lds, st>>>(a);
   return launched();
+}
+
+// Which kernel a product of more than 16 tokens takes, by estimates in microseconds.
+//   split, TM = 1 or 2 token tiles of 32: 3 us, and the longest of what its work-groups read at 12 MB/us (L2), of
+//     one's own reading at 45 KB/us and of the weights at 5 MB/us (memory);
+//   gemm, 256 rows (gated 128 of each) x 32 TM tokens, TM = 1 .. 4: 5.5 us, and the longer of its chunks and of the
+//     weights at 4.5 MB/us.  A chunk takes a work-group alone on its compute unit {0.15, 0.20, 0.28, 0.36} us,
+//     several {0.20, 0.31, 0.40, 0.50} each.
+// Measured, split 1 / split 2 / gemm of TM = 1, 2, 3, 4 (us): linear of 77 tokens, 5120 x 5120: 9.9 / 10.1 / 11.3, 12.9,
+// 17.8, 21.0; of 256: 19.8 / 17.9 / 11.5, 13.4, 17.5, 20.6; of 64, 5120 x 13824: 17.6 / 20.7 / -, 33.8; of 1000: 108 / 108
+// / 72, 53.6, 46.8, 58.7; of 2000: - / - / 137, 94.9, 81.1, 89.6; gated of 77, 13824 x 5120: 45 / 34 / -, 23, 28, 33; of
+// 2000: - / - / -, 189, 159, 154.
+struct Choice {
+  bool split;
+  int tm;
+};
+Choice choose(int64_t m, int64_t n, int64_t k, int mats) {
+  static const double alone[4] = {0.15, 0.20, 0.28, 0.36}, shared[4] = {0.20, 0.31, 0.40, 0.50};
+  const double row = static_cast<double>(tile_bytes(static_cast<int>(k))) / kRows, weights = row * n * mats;
+  const int64_t chunks = chunks_of(static_cast<int>(k));
+  Choice best = {true, 1};
+  double least = 0;
+  for (int tm = 1; tm <= 2; ++tm) {
+    const int64_t groups = (n + 31) / 32 * ((m + 32 * tm - 1) / (32 * tm));
+    const double bytes = row * 32 * (mats + tm);
+    const double t = 3 + std::max({groups * bytes / 12e6, std::max(1.0, groups / 256.0) * bytes / 45e3, weights / 5e6});
+    if (tm == 1 || t < least) least = t, best = {true, tm};
+  }
+  if (m <= 32) return {true, 1};
+  for (int tm = 1; tm <= 4; ++tm) {
+    const int64_t groups = (n * mats + 255) / 256 * ((m + 32 * tm - 1) / (32 * tm)), each = (groups + 255) / 256;
+    const double t = 5.5 + std::max(chunks * (each == 1 ? alone[tm - 1] : each * shared[tm - 1]), weights / 4.5e6);
+    if (t <= least) least = t, best = {false, tm};
+  }
+  return best;
 }
 
 template <int MODE>
@@ -414,9 +554,12 @@ polyq_status run(const Args& a, hipStream_t st) {
     if (a.x_type == POLYQ_MX_BF16) return run_raw<MODE, __bf16>(a, st);
     if (a.m <= 16) return run_stream<MODE, Packed, true>(a, st);
   }
-  const int64_t tiles = static_cast<int64_t>(tiles_of(a.n)) * (MODE == kLinear ? 1 : 2) * tiles_of(a.m);
-  if (tiles >= 128 * 128) return run_gemm<MODE, 4, 1, 2, 4>(a, st);
-  return run_gemm<MODE, 4, 1, 2, 2>(a, st);
+  const Choice c = choose(a.m, a.n, a.k, MODE == kLinear ? 1 : 2);
+  if (c.split) return c.tm == 1 ? run_split<MODE, 1, 8>(a, st) : run_split<MODE, 2, MODE == kLinear ? 8 : 4>(a, st);
+  if (c.tm == 1) return run_gemm<MODE, 4, 1, 2, 1, 4>(a, st);
+  if (c.tm == 2) return run_gemm<MODE, 4, 1, 2, 2, 4>(a, st);
+  if (c.tm == 3) return run_gemm<MODE, 4, 1, 2, 3, 2>(a, st);
+  return run_gemm<MODE, 4, 1, 2, 4, 2>(a, st);
 }
 
 }  // namespace

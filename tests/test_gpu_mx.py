@@ -176,6 +176,70 @@ def test_linear(m, n, k, t):
     within(y32, want, sum_tol(mag, k) + out_tol(want, torch.float32), "linear fp32")
 
 
+def device_linear(x, w):
+    """q(x) q(w)^T and the sums of magnitudes in 64 bits on the GPU, from the operators' own quantization (checked
+    against the definition above): for shapes too large for the CPU."""
+    xv, wv = (pq.mx_dequantize(pq.mx_quantize(v)).double() for v in (x, w))
+    return xv, wv, xv @ wv.T, xv.abs() @ wv.abs().T
+
+
+# Shapes that reach every kernel and tile of the products: (17 .. 64 tokens: K split over waves; more: tiles of 32, 64,
+# 96 and 128 tokens), each with whole tiles, ragged ones, and records that end early.
+TILES = [(17, 700, 2000), (40, 5120, 1100), (64, 13824, 520), (200, 8192, 1152), (300, 2050, 640), (520, 5120, 1408),
+         (700, 5001, 640), (1000, 13824, 384), (1500, 5120, 640), (2000, 5120, 1280), (2050, 13824, 260)]
+
+
+@pytest.mark.parametrize("m,n,k", TILES)
+def test_linear_tiles(m, n, k):
+    g = torch.Generator(device=dev()).manual_seed(m)
+    x = torch.randn((m, k), generator=g, device=dev()).bfloat16()
+    w = torch.randn((n, k), generator=g, device=dev()) * 0.05
+    _, _, want, mag = device_linear(x, w)
+    wq = pq.mx_quantize(w)
+    for typ in (torch.float32, torch.bfloat16):
+        y = pq.mx_linear(x, wq, dtype=typ)
+        tol = sum_tol(mag, k) + out_tol(want, typ)
+        assert bool(((y.double() - want).abs() <= tol).all()), (typ, m, n, k)
+
+
+@pytest.mark.parametrize("m,n,k", TILES)
+def test_gated_tiles(m, n, k):
+    g = torch.Generator(device=dev()).manual_seed(m)
+    x = torch.randn((m, k), generator=g, device=dev()).bfloat16()
+    gate, up = (torch.randn((n, k), generator=g, device=dev()) * 0.05 for _ in range(2))
+    _, _, gw, gm = device_linear(x, gate)
+    _, _, uw, um = device_linear(x, up)
+    a = act64("silu", gw)[0]
+    ea, eu = 1.2 * sum_tol(gm, k) + act_tol(gw, a), sum_tol(um, k)
+    want = a * uw
+    tol = (ea * uw.abs() + (a.abs() + ea) * eu + 2.0 ** -23 * want.abs()) * (1 + 2.0 ** -8)
+    gq, uq = pq.mx_quantize(gate), pq.mx_quantize(up)
+    for typ in (torch.float32, torch.bfloat16):
+        h = pq.mx_gated(x, gq, uq, dtype=typ)
+        assert bool(((h.double() - want).abs() <= tol + out_tol(want, typ)).all()), (typ, m, n, k)
+
+
+# Shapes that reach every tile of the gradients' products: 256 x 256, 256 x 128 (few tokens) and 256 x 64, with and
+# without a split reduction.
+GRADS = [(64, 8192, 4096), (40, 5120, 2000), (300, 4100, 4352), (1100, 2200, 5120), (2000, 1000, 5120), (520, 13824, 640)]
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("m,n,k", GRADS)
+def test_linear_backward_tiles(m, n, k, t):
+    g = torch.Generator(device=dev()).manual_seed(m)
+    x = torch.randn((m, k), generator=g, device=dev()).to(F[t])
+    w = torch.randn((n, k), generator=g, device=dev()) * 0.05
+    dy = torch.randn((m, n), generator=g, device=dev()).to(F[t])
+    xv, wv, _, _ = device_linear(x, w)
+    d = dy.double()
+    terms = {"bf16": 1, "fp32": 3}[t]
+    for got, want, mag, length in zip(pq.mx_linear_backward(dy, x, pq.mx_quantize(w)), (d @ wv, d.T @ xv),
+                                      (d.abs() @ wv.abs(), d.abs().T @ xv.abs()), (n, m)):
+        tol = 2.0 ** -23 * (terms * (length // 32 + 2) + 40) * mag + out_tol(want, F[t])
+        assert bool(((got.double() - want).abs() <= tol).all()), (t, m, n, k)
+
+
 def act64(act, g):
     if act == "silu":
         s = torch.sigmoid(g)
