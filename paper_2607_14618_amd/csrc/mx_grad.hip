@@ -117,7 +117,7 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   // L of dx: packed fragments (16 r x 128 l) into registers, and from there as bf16 into LDS.
   const int chunks = chunks_of(g.k), b_tiles = tiles_of(g.n);
   i4v codes[FRAGS];
-  uint32_t bytes[FRAGS];
+  uint32_t words[FRAGS];  // the scales of the fragment's record
   const uint8_t *w0 = g.w[0], *w1 = g.w[1];
   int tile0 = 0;  // the first row tile of the stage in `codes`
   auto fetch_codes = [&](const Place& p) {
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
       const int c = min(lb * (L / kChunk) + f / (kStep / kRows), chunks - 1);
       const uint8_t* src = w + tile * tb;
       codes[i] = *reinterpret_cast<const i4v*>(src + chunk_offset(c) + lane * 16);
-      bytes[i] = src[scale_offset(c) + lane * 4 + (c & 3)];
+      words[i] = *reinterpret_cast<const uint32_t*>(src + scale_offset(c) + lane * 4);
     }
   };
   auto convert = [&](int half, auto which) {  // half H of each fragment's 32 channels per lane
@@ -138,7 +138,8 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
     for (int i = 0; i < FRAGS; ++i) {
       const int f = i * W + wave, rt = f % (kStep / kRows);
       const bool there = tile0 + rt < b_tiles;  // rows behind the last tile are zeros
-      const float s = scale_value(there ? bytes[i] : 127u);
+      const int c = min(lb * (L / kChunk) + f / (kStep / kRows), chunks - 1);
+      const float s = scale_value(there ? (words[i] >> (8 * (c & 3))) & 255u : 127u);
       uint32_t v[8];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
