@@ -205,6 +205,45 @@ __device__ __forceinline__ void store_pair(T* to, f4 a, f4 b, int upper) {
     *reinterpret_cast<u4v*>(to + upper * 4) = pack_halves(p, q);
   }
 }
+// 32 rows x 64 columns of an output, two 32x32 products side by side whose lane l has row l % 32 and columns 8 r + 4 (l
+// / 32) .. + 3 in elements 4 r .. of each, by way of a wave's own 4 or 8 KiB of LDS to rows of `pitch` elements at
+// `out`, in pieces of 16 bytes of which 8 or 16 lanes make a row: a store then touches 8 or 4 rows and not 32.
+// Only pieces of rows < rows_left and columns < cols_left are written; every piece is all there or not at all, and on
+// 16 bytes.  Pieces are swizzled by row so that neighbouring rows fall into different banks.
+template <class T>
+__device__ __forceinline__ void store_rows(uint8_t* lds, T* out, int64_t pitch, const f16v& a, const f16v& b, int lane,
+                                           int rows_left, int cols_left) {
+  constexpr int UNITS = 64 * sizeof(T) / 16, PER = 16 / sizeof(T);  // pieces of a row, elements of a piece
+  const int row = lane & 31, upper = lane >> 5;
+  uint8_t* mine = lds + row * (UNITS * 16);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const f16v& d = t == 0 ? a : b;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f4*>(mine + (((t * 8 + r * 2 + upper) ^ (row & 7)) * 16)) =
+            f4{d[4 * r], d[4 * r + 1], d[4 * r + 2], d[4 * r + 3]};
+    } else {
+      typedef T t4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        t4 p, q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = static_cast<T>(d[4 * r + i]), q[i] = static_cast<T>(d[4 * r + 4 + i]);
+        *reinterpret_cast<u4v*>(mine + (((t * 4 + r + upper) ^ (row & 7)) * 16)) = pack_halves(p, q);
+      }
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int s = 0; s < UNITS / 2; ++s) {
+    const int at = s * (64 / UNITS) + lane / UNITS, unit = lane % UNITS;
+    const u4v v = *reinterpret_cast<const u4v*>(lds + at * (UNITS * 16) + (unit ^ (at & 7)) * 16);
+    if (at < rows_left && unit * PER < cols_left) *reinterpret_cast<u4v*>(out + at * pitch + unit * PER) = v;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
 // The same with the type known at run time.
 __device__ __forceinline__ f4 load4(const void* base, int type, int64_t at, bool vec, int valid) {
   if (type == POLYQ_MX_F32) return load4(static_cast<const float*>(base) + at, vec, valid);

@@ -263,6 +263,19 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
     T* base = static_cast<T*>(g.splits > 1 ? static_cast<void*>(g.part + (static_cast<int64_t>(blockIdx.y) * (DW ? g.mats : 1) + mat_out) *
                                                                               g.rows * g.k)
                                            : (mat_out ? g.out[1] : g.out[0]));
+    if (vec16) {  // pairs of tiles side by side, by way of LDS
+      uint8_t* room = lds + wave * 8192;
+#pragma unroll
+      for (int o = 0; o < (DW ? TL : TS); ++o)
+#pragma unroll
+        for (int c = 0; c < (DW ? TS : TL); c += 2) {
+          const int row = (DW ? (lb * WL + wl) * TL + o : (sb * WS + ws) * TS + o) * 32;
+          const int col = (DW ? (sb * WS + ws) * TS + c : (lb * WL + wl) * TL + c) * 32;
+          store_rows(room, base + static_cast<int64_t>(row) * g.k + col, g.k, DW ? acc[o][c] : acc[c][o],
+                     DW ? acc[o][c + 1] : acc[c + 1][o], lane, g.rows - row, g.k - col);
+        }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TL; ++i)
 #pragma unroll
@@ -270,21 +283,14 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
         const int lt = (lb * WL + wl) * TL + i, st = (sb * WS + ws) * TS + j;
         const int row = (DW ? lt : st) * 32 + (lane & 31), col = (DW ? st : lt) * 32 + (lane >> 5) * 4;
         if (row >= g.rows) continue;
-        T* to = base + static_cast<int64_t>(row) * g.k + col;
-        const f16v& d = acc[i][j];
 #pragma unroll
-        for (int r = 0; r < 4; r += 2) {
-          const f4 v = {d[4 * r], d[4 * r + 1], d[4 * r + 2], d[4 * r + 3]};
-          const f4 v8 = {d[4 * r + 4], d[4 * r + 5], d[4 * r + 6], d[4 * r + 7]};
-          if (vec16) {  // k is a multiple of 16: all of the two groups and of both halves' is there, or none
-            if (col + r * 8 < g.k) store_pair(to + r * 8, v, v8, lane >> 5);
-          } else {
-            if (col + r * 8 < g.k) store4(to + r * 8, v, vec, g.k - col - r * 8);
-            if (col + r * 8 + 8 < g.k) store4(to + r * 8 + 8, v8, vec, g.k - col - r * 8 - 8);
-          }
-        }
+        for (int r = 0; r < 4; ++r)
+          if (col + r * 8 < g.k)
+            store4(base + static_cast<int64_t>(row) * g.k + col + r * 8,
+                   f4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]}, vec, g.k - col - r * 8);
       }
   };
+  __syncthreads();  // every wave has read the last of its L
   if (g.splits > 1 || g.type == POLYQ_MX_F32) out(F32());
   else if (g.type == POLYQ_MX_F16) out(F16());
   else out(BF16());
@@ -361,15 +367,13 @@ inline int64_t pad64(int64_t v) { return align_up(v, 64); }
 
 // One gradient product's tile and splits: outputs of `l` by `s`, `stages` of the reduction.
 struct Shape {
-  int tile;  // of l x s: 256 x 256 by eight waves, 256 x 128 and 256 x 64 by four
+  int tile;  // 256 x 256 of l x s by eight waves, or 256 x 64 by four
   int l_blocks, s_blocks, splits;
 };
-Shape grad_shape(bool dw, int l, int s, int outs, int stages) {
+Shape grad_shape(int l, int s, int outs, int stages) {
   Shape h;
   const int64_t big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs;
-  // Few tokens make short sums for dW: two work-groups a compute unit then, one's stores behind the other's
-  // products (64 tokens, 5120 x 5120: 23 us instead of 31; of 2000 tokens 285 and 294, 564 and 526 gated).
-  h.tile = big < 128 ? 64 : dw && stages <= 16 ? 128 : 256;
+  h.tile = big < 128 ? 64 : 256;
   h.l_blocks = div_up(l, 256), h.s_blocks = div_up(s, h.tile);
   const int64_t groups = static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs;
   // Work-groups that run at once.  The reduction is split where rounds of whole tiles leave much of the GPU idle; a
@@ -401,12 +405,11 @@ polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
 template <bool DW>
 polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
   const int outs = DW ? g.mats : 1, stages = g.terms * g.rsteps * (DW ? 1 : g.mats);
-  const Shape h = DW ? grad_shape(true, g.n, g.k, outs, stages) : grad_shape(false, g.k, g.m, outs, stages);
+  const Shape h = DW ? grad_shape(g.n, g.k, outs, stages) : grad_shape(g.k, g.m, outs, stages);
   g.splits = h.splits, g.l_blocks = h.l_blocks, g.s_blocks = h.s_blocks;
   g.part = static_cast<float*>(part);
   const polyq_status r = h.tile == 256 ? run_tile<DW, 2, 4, 4, 2>(g, outs, st)
-                         : DW && h.tile == 128 ? run_tile<DW, 2, 2, 4, 2>(g, outs, st)
-                                               : run_tile<DW, 4, 1, 2, 2>(g, outs, st);
+                                          : run_tile<DW, 4, 1, 2, 2>(g, outs, st);
   if (r != POLYQ_OK || h.splits == 1) return r;
   const int64_t blocks = (static_cast<int64_t>(g.rows) * g.k + 1023) / 1024;
   mx_grad_sum_kernel<<<dim3(static_cast<uint32_t>(blocks), outs), dim3(256), 0, st>>>(g);
@@ -429,11 +432,11 @@ GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int gr
   p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
   p.part_bytes = 0;
   if (dx) {
-    const Shape s = grad_shape(false, k, m, 1, p.terms * mats * (p.n_pad / kStep));
+    const Shape s = grad_shape(k, m, 1, p.terms * mats * (p.n_pad / kStep));
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * m * k * 4);
   }
   if (dw) {
-    const Shape s = grad_shape(true, n, k, mats, p.terms * (p.m_pad / kStep));
+    const Shape s = grad_shape(n, k, mats, p.terms * (p.m_pad / kStep));
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * mats * n * k * 4);
   }
   p.total = p.x_bytes + p.plane_bytes + p.xt_bytes + p.part_bytes;
