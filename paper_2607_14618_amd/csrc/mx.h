@@ -287,6 +287,36 @@ __device__ __forceinline__ bf16x8 read_transposed(const uint8_t* p, int next = 1
   return u.v;
 }
 
+constexpr int kBlockBytes = 1024;  // 32 x 16 bf16
+
+// A fragment (16 tokens x 128 channels) as four bf16 blocks of 32 channels x 16 tokens, rows of 32 bytes, at
+// [channel / 32][tile]: the lanes convert 32 values each into a wave's own 4 KiB of LDS, blocks of 16 tokens x 32
+// channels, and read them transposed.
+__device__ __forceinline__ void transpose_chunk(uint8_t* lds, i4v codes, uint32_t byte, int lane, uint8_t* out, int chunk,
+                                                int tile, int m_tiles, int c_tiles) {
+  const float s = scale_value(byte);
+  uint8_t* block = lds + (lane >> 4) * kBlockBytes;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t code = static_cast<uint32_t>(codes[w]);
+    const u4v v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
+    *reinterpret_cast<u4v*>(block + (lane & 15) * 64 + w * 16) = v;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // Lane group h = lane / 16 of a block: channels 16 (h & 1) .. + 15, tokens 8 (h >> 1) .. + 7.
+  const int i = lane & 15, half = (lane >> 4) & 1, upper = lane >> 5;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int ct = chunk * 4 + q;
+    const bf16x8 v = read_transposed(lds + q * kBlockBytes + (upper * 8 + (i >> 2)) * 64 + half * 32 + (i & 3) * 8, 4 * 64);
+    if (ct < c_tiles)
+      *reinterpret_cast<bf16x8*>(out + (static_cast<int64_t>(ct) * m_tiles + tile) * kBlockBytes + (half * 16 + i) * 32 + upper * 16) = v;
+  }
+}
+
 // ------------------------------------------------------------------ activations
 // act(g) and, if asked for, act'(g), in fp32:
 //   silu       g s,  s = 1 / (1 + exp(-g));        s (1 + g (1 - s))
@@ -339,8 +369,10 @@ inline bool valid_shape(int32_t rows, int32_t k) {
 }
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-// x [rows][k] into the packed layout (arguments checked by the caller).
-polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, void* packed, hipStream_t st);
+// x [rows][k] into the packed layout and, if asked for, into transposed blocks (transpose_chunk; rows padded to 64);
+// either may be null (arguments checked by the caller).
+polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, void* packed, hipStream_t st,
+                             void* transposed = nullptr);
 
 // dg and du of the gated block as bf16 planes [terms][2][m_pad][n_pad] in blocks (plane_at; zero behind m and
 // n), whose sum over the terms is the fp32 value: to 2^-9, 2^-17 and 2^-25 of it with one,

@@ -26,7 +26,6 @@ namespace {
 // S is stored in memory as blocks of 32 s x 16 r, which are the operand fragments of a
 // wave, and goes from there into registers.
 constexpr int kStep = 64;            // r of a stage
-constexpr int kBlockBytes = 1024;    // 32 x 16 bf16
 constexpr int kMaxRows = 1 << 21;    // tokens and output channels: a work-group's S is reached with 32-bit offsets
 
 struct GradArgs {
@@ -296,9 +295,8 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   else out(BF16());
 }
 
-// x^ [m][k], packed, as bf16 blocks of 32 channels x 16 tokens, [c_tiles][m_pad / 16], zero
-// behind m and k.  A wave takes a chunk of a tile: its lanes convert 32 values each into LDS,
-// 4 blocks of 16 tokens x 32 channels, and read them transposed.
+// x^ [m][k], packed, as bf16 blocks of 32 channels x 16 tokens, [c_tiles][m_pad / 16], zero behind m and k: a wave takes
+// a chunk of a tile.  (Activations that come in their own type leave the quantization in both forms.)
 __global__ __launch_bounds__(256) void mx_transpose_kernel(const uint8_t* __restrict__ packed, uint8_t* __restrict__ out, int m,
                                                            int k, int m_tiles, int c_tiles, int64_t jobs) {
   __shared__ uint8_t lds[4][4 * kBlockBytes];
@@ -306,34 +304,14 @@ __global__ __launch_bounds__(256) void mx_transpose_kernel(const uint8_t* __rest
   const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + wave;
   if (job >= jobs) return;  // waves are independent: no barrier follows
   const int chunks = chunks_of(k), tile = static_cast<int>(job / chunks), chunk = static_cast<int>(job % chunks);
-  const bool there = tile * kRows < m;
-  const uint8_t* src = packed + min(tile, tiles_of(m) - 1) * tile_bytes(k);
-  const i4v codes = *reinterpret_cast<const i4v*>(src + chunk_offset(chunk) + lane * 16);
-  const uint32_t byte = src[scale_offset(chunk) + lane * 4 + (chunk & 3)];
-  const float s = scale_value(byte);
-  uint8_t* block = lds[wave] + (lane >> 4) * kBlockBytes;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const uint32_t code = static_cast<uint32_t>(codes[w]);
-    u4v v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)),
-             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
-             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
-             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
-    if (!there) v = u4v{0, 0, 0, 0};
-    *reinterpret_cast<u4v*>(block + (lane & 15) * 64 + w * 16) = v;
+  i4v codes = {0, 0, 0, 0};
+  uint32_t byte = 127;
+  if (tile * kRows < m) {
+    const uint8_t* src = packed + tile * tile_bytes(k);
+    codes = *reinterpret_cast<const i4v*>(src + chunk_offset(chunk) + lane * 16);
+    byte = src[scale_offset(chunk) + lane * 4 + (chunk & 3)];
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  // Lane group h = lane / 16 of a block: channels 16 (h & 1) .. + 15, tokens 8 (h >> 1) .. + 7.
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int ct = chunk * 4 + q;
-    const int i = lane & 15;
-    const uint8_t* p = lds[wave] + q * kBlockBytes + ((lane >> 5) * 8 + (i >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
-    const bf16x8 v = read_transposed(p, 4 * 64);
-    if (ct < c_tiles)
-      *reinterpret_cast<bf16x8*>(out + (static_cast<int64_t>(ct) * m_tiles + tile) * kBlockBytes + (((lane >> 4) & 1) * 16 + i) * 32 +
-                                 (lane >> 5) * 16) = v;
-  }
+  transpose_chunk(lds[wave], codes, byte, lane, out, chunk, tile, m_tiles, c_tiles);
 }
 
 // Adds the splits' sums in order.
@@ -424,10 +402,11 @@ struct GradPlan {
   size_t x_bytes, plane_bytes, xt_bytes, part_bytes, total;
 };
 GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int grad_type, bool dx, bool dw) {
+  // the packed x is what g and u are computed from; the linear layer's gradients need the transposed one alone
   GradPlan p;
   p.terms = grad_type == POLYQ_MX_BF16 ? 1 : grad_type == POLYQ_MX_F16 ? 2 : 3;
   p.m_pad = static_cast<int32_t>(pad64(m)), p.n_pad = static_cast<int32_t>(pad64(n));
-  p.x_bytes = x_type == POLYQ_MX_PACKED ? 0 : align_up(static_cast<int64_t>(polyq_mx_bytes(m, k)), 256);
+  p.x_bytes = x_type == POLYQ_MX_PACKED || mats == 1 ? 0 : align_up(static_cast<int64_t>(polyq_mx_bytes(m, k)), 256);
   p.plane_bytes = static_cast<size_t>(p.terms) * p.m_pad * mats * p.n_pad * 2;
   p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
   p.part_bytes = 0;
@@ -471,13 +450,13 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
   if (!aligned(ws, 256)) return POLYQ_ERR_ARG;
   uint8_t* at = static_cast<uint8_t*>(ws);
   const void* x = q.x;
-  if (p.x_bytes > 0) {
-    const polyq_status s = launch_quantize(q.x, q.x_type, q.m, q.k, at, st);
+  void* planes = at + p.x_bytes;
+  uint8_t* xt = at + p.x_bytes + p.plane_bytes;
+  if (need_x && q.x_type != POLYQ_MX_PACKED) {
+    const polyq_status s = launch_quantize(q.x, q.x_type, q.m, q.k, p.x_bytes > 0 ? at : nullptr, st, dw ? xt : nullptr);
     if (s != POLYQ_OK) return s;
     x = at;
   }
-  void* planes = at + p.x_bytes;
-  uint8_t* xt = at + p.x_bytes + p.plane_bytes;
   void* part = xt + p.xt_bytes;
   if (q.act >= 0) {
     const polyq_status s = launch_gated_grad(q.w[0], q.w[1], x, q.d, q.d_type, q.m, q.n, q.k, q.act, planes, p.terms,
@@ -505,12 +484,14 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
     if (s != POLYQ_OK) return s;
   }
   if (dw) {
-    const int m_tiles = p.m_pad / 16, c_tiles = div_up(q.k, 32);
-    const int64_t jobs = static_cast<int64_t>(m_tiles) * chunks_of(q.k), blocks = (jobs + 3) / 4;
-    mx_transpose_kernel<<<dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st>>>(static_cast<const uint8_t*>(x), xt, q.m, q.k,
-                                                                                  m_tiles, c_tiles, jobs);
-    const polyq_status s = launched();
-    if (s != POLYQ_OK) return s;
+    if (q.x_type == POLYQ_MX_PACKED) {
+      const int m_tiles = p.m_pad / 16, c_tiles = div_up(q.k, 32);
+      const int64_t jobs = static_cast<int64_t>(m_tiles) * chunks_of(q.k), blocks = (jobs + 3) / 4;
+      mx_transpose_kernel<<<dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st>>>(static_cast<const uint8_t*>(x), xt, q.m, q.k,
+                                                                                    m_tiles, c_tiles, jobs);
+      const polyq_status s = launched();
+      if (s != POLYQ_OK) return s;
+    }
     g.out[0] = q.dw[0], g.out[1] = q.dw[1], g.rows = q.n, g.rsteps = p.m_pad / kStep;
     g.vec = q.k % 4 == 0 && aligned(q.dw[0], 4 * size) && aligned(q.dw[1], 4 * size);
     g.vec16 = q.k % 16 == 0 && aligned(q.dw[0], 16) && aligned(q.dw[1], 16);

@@ -22,10 +22,13 @@ namespace {
 
 constexpr int kWaves = 4, kWaveRows = kRows / kWaves;
 
-template <class T, bool VEC>
+// packed, or XT and then xt too: the values once more as transposed blocks, for the weights' gradients.
+template <class T, bool VEC, bool XT>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_kernel(const T* __restrict__ x, uint8_t* __restrict__ packed,
-                                                                  int rows, int k, int records) {
+                                                                  uint8_t* __restrict__ xt, int rows, int k, int records,
+                                                                  int m_tiles) {
   __shared__ Record r;
+  __shared__ uint8_t blocks[XT ? kWaves : 1][4 * kBlockBytes];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tile = static_cast<int>(blockIdx.x / records), rec = static_cast<int>(blockIdx.x % records);
   const int k0 = rec * kRec + lane * 8, row0 = tile * kRows + wave * kWaveRows;
@@ -46,9 +49,16 @@ __global__ __launch_bounds__(64 * kWaves) void mx_quantize_kernel(const T* __res
     if ((lane & 3) == 0) *r.scale(wave * kWaveRows + u, lane) = static_cast<uint8_t>(none ? 127u : byte);
   }
   __syncthreads();
-  uint8_t* out = packed + tile * tile_bytes(k) + static_cast<int64_t>(rec) * kRecBytes;
-  if (wave < chunks_of(k) - rec * 4) *reinterpret_cast<u4v*>(out + kScaleBytes + wave * kChunkBytes + lane * 16) = *r.fragment(wave, lane);
-  if (wave == 0) reinterpret_cast<uint32_t*>(out)[lane] = reinterpret_cast<const uint32_t*>(r.scales)[lane];
+  const bool there = wave < chunks_of(k) - rec * 4;
+  const u4v codes = *r.fragment(wave, lane);
+  if (!XT || (packed != nullptr && tile * kRows < rows)) {
+    uint8_t* out = packed + tile * tile_bytes(k) + static_cast<int64_t>(rec) * kRecBytes;
+    if (there) *reinterpret_cast<u4v*>(out + kScaleBytes + wave * kChunkBytes + lane * 16) = codes;
+    if (wave == 0) reinterpret_cast<uint32_t*>(out)[lane] = reinterpret_cast<const uint32_t*>(r.scales)[lane];
+  }
+  if (XT && there)
+    transpose_chunk(blocks[XT ? wave : 0], __builtin_bit_cast(i4v, codes), r.scales[lane * 4 + wave], lane, xt, rec * 4 + wave, tile,
+                    m_tiles, div_up(k, 32));
 }
 
 template <class T, bool VEC>
@@ -159,29 +169,25 @@ polyq_status check_jobs(int64_t groups) { return groups > 0x7FFFFFFFll ? POLYQ_E
 
 polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
 
+template <class T>
+polyq_status quantize(const T* x, int32_t rows, int32_t k, uint8_t* packed, uint8_t* xt, hipStream_t st) {
+  const int records = records_of(k), tiles = xt ? static_cast<int>(align_up(rows, 64) / kRows) : tiles_of(rows);
+  const int64_t groups = static_cast<int64_t>(tiles) * records;
+  if (check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
+  const bool vec = aligned(x, 16) && static_cast<int64_t>(k) * sizeof(T) % 16 == 0;
+  const auto kernel = xt ? (vec ? mx_quantize_kernel<T, true, true> : mx_quantize_kernel<T, false, true>)
+                         : (vec ? mx_quantize_kernel<T, true, false> : mx_quantize_kernel<T, false, false>);
+  kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(64 * kWaves), 0, st>>>(x, packed, xt, rows, k, records, tiles);
+  return launched();
+}
+
 }  // namespace
 
-polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, void* packed, hipStream_t st) {
-  const int records = records_of(k);
-  const int64_t groups = static_cast<int64_t>(tiles_of(rows)) * records;
-  if (check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
-  const bool vec = aligned(x, 16) && static_cast<int64_t>(k) * type_bytes(type) % 16 == 0;
-  uint8_t* out = static_cast<uint8_t*>(packed);
-  const dim3 grid(static_cast<uint32_t>(groups)), block(64 * kWaves);
-#define POLYQ_MX_QUANTIZE(T)                                                                                        \
-  if (vec)                                                                                                          \
-    mx_quantize_kernel<T, true><<<grid, block, 0, st>>>(static_cast<const T*>(x), out, rows, k, records);      \
-  else                                                                                                              \
-    mx_quantize_kernel<T, false><<<grid, block, 0, st>>>(static_cast<const T*>(x), out, rows, k, records)
-  if (type == POLYQ_MX_F32) {
-    POLYQ_MX_QUANTIZE(float);
-  } else if (type == POLYQ_MX_F16) {
-    POLYQ_MX_QUANTIZE(_Float16);
-  } else {
-    POLYQ_MX_QUANTIZE(__bf16);
-  }
-#undef POLYQ_MX_QUANTIZE
-  return launched();
+polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, void* packed, hipStream_t st, void* transposed) {
+  uint8_t *out = static_cast<uint8_t*>(packed), *xt = static_cast<uint8_t*>(transposed);
+  if (type == POLYQ_MX_F32) return quantize(static_cast<const float*>(x), rows, k, out, xt, st);
+  if (type == POLYQ_MX_F16) return quantize(static_cast<const _Float16*>(x), rows, k, out, xt, st);
+  return quantize(static_cast<const __bf16*>(x), rows, k, out, xt, st);
 }
 
 }  // namespace mx
