@@ -45,8 +45,9 @@ struct GradArgs {
   int32_t vec16;        // k is a multiple of 16 and the outputs are on 16 bytes
 };
 
-// WL x WS waves, each TL x 32 l by TS x 32 s.
-template <bool DW, int WL, int WS, int TL, int TS>
+// WL x WS waves, each TL x 32 l by TS x 32 s.  TERMS: planes of d that a stage of dx multiplies the one W by; more
+// terms than that are further stages.
+template <bool DW, int WL, int WS, int TL, int TS, int TERMS>
 __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs g) {
   constexpr int W = WL * WS, L = WL * TL * 32, S = WS * TS * 32;
   constexpr int STAGE = L * kStep * 2;
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   const int64_t tb = tile_bytes(g.k);
 
   // Stages: terms x (DW ? 1 : mats) x rsteps, split evenly.
-  const int stages = g.terms * g.rsteps * (DW ? 1 : g.mats);
+  const int stages = g.terms / TERMS * g.rsteps * (DW ? 1 : g.mats);
   const int first = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / g.splits);
   const int last = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / g.splits);
 
@@ -86,14 +87,17 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   for (int i = 0; i < TS; ++i)
     so[i] = static_cast<uint32_t>(min(sb * (S / 32) + ws * TS + i, s_tiles - 1) - s0) * static_cast<uint32_t>(s_tile) +
             (lane & 31) * 32 + (lane >> 5) * 16;
-  i4v sf[4][TS];
+  i4v sf[4][TERMS][TS];
   auto load_s = [&](const Place& p, auto which) {  // the fragments of step J of a stage
     constexpr int J = decltype(which)::value;
-    const uint8_t* base = (DW ? g.xt : g.d + p.plane * g.plane) + s0 * s_tile;
-    const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, (s_tiles - s0) * s_tile);
 #pragma unroll
-    for (int i = 0; i < TS; ++i)
-      sf[J][i] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(buf, so[i], (p.r * 4 + J) * kBlockBytes, 0));
+    for (int t = 0; t < TERMS; ++t) {
+      const uint8_t* base = (DW ? g.xt : g.d + (p.plane + t * g.mats) * g.plane) + s0 * s_tile;
+      const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, (s_tiles - s0) * s_tile);
+#pragma unroll
+      for (int i = 0; i < TS; ++i)
+        sf[J][t][i] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(buf, so[i], (p.r * 4 + J) * kBlockBytes, 0));
+    }
   };
 
   // L of dW: whole blocks by way of registers.
@@ -174,13 +178,15 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   auto multiply = [&](auto which) {  // rows of D: the output's columns c
     constexpr int J = decltype(which)::value;
 #pragma unroll
-    for (int j = 0; j < TS; ++j) {
-      const bf16x8 sv = __builtin_bit_cast(bf16x8, sf[J][j]);
+    for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-      for (int i = 0; i < TL; ++i)
-        acc[i][j] = DW ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(sv, lf[J & 1][i], acc[i][j], 0, 0, 0)
-                       : __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf[J & 1][i], sv, acc[i][j], 0, 0, 0);
-    }
+      for (int j = 0; j < TS; ++j) {
+        const bf16x8 sv = __builtin_bit_cast(bf16x8, sf[J][t][j]);
+#pragma unroll
+        for (int i = 0; i < TL; ++i)
+          acc[i][j] = DW ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(sv, lf[J & 1][i], acc[i][j], 0, 0, 0)
+                         : __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf[J & 1][i], sv, acc[i][j], 0, 0, 0);
+      }
   };
   typedef std::integral_constant<int, 0> I0;
   typedef std::integral_constant<int, 1> I1;
@@ -348,15 +354,17 @@ struct Shape {
   int tile;  // 256 x 256 of l x s by eight waves, or 256 x 64 by four
   int l_blocks, s_blocks, splits;
 };
-Shape grad_shape(int l, int s, int outs, int stages) {
+// `steps` stages of each of `terms`; `shared`: the small tile takes all terms in one stage.
+Shape grad_shape(int l, int s, int outs, int steps, int terms, bool shared) {
   Shape h;
   const int64_t big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs;
   h.tile = big < 128 ? 64 : 256;
   h.l_blocks = div_up(l, 256), h.s_blocks = div_up(s, h.tile);
   const int64_t groups = static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs;
-  // Work-groups that run at once.  The reduction is split where rounds of whole tiles leave much of the GPU idle; a
-  // split costs its partial sums, about as much as 8 stages, and has at least 8.
-  const int slots = h.tile == 256 ? 256 : 512;
+  const int stages = shared && h.tile == 64 ? steps : steps * terms;
+  // Work-groups that run at once: one or two per compute unit.  The reduction is split where rounds of whole tiles
+  // leave much of the GPU idle; a split costs its partial sums, about as much as 8 stages, and has at least 8.
+  const int slots = h.tile == 256 ? kCUs : 2 * kCUs;
   h.splits = 1;
   int64_t best = -1;
   for (int n = 1; n <= 32 && (n == 1 || stages / n >= 8); ++n) {
@@ -366,10 +374,10 @@ Shape grad_shape(int l, int s, int outs, int stages) {
   return h;
 }
 
-template <bool DW, int WL, int WS, int TL, int TS>
+template <bool DW, int WL, int WS, int TL, int TS, int TERMS>
 polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
   const size_t lds = 2 * static_cast<size_t>(WL * TL * 32) * kStep * 2;
-  const auto kernel = mx_grad_kernel<DW, WL, WS, TL, TS>;
+  const auto kernel = mx_grad_kernel<DW, WL, WS, TL, TS, TERMS>;
   if (lds > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(lds)) != hipSuccess)
@@ -382,12 +390,14 @@ polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
 
 template <bool DW>
 polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
-  const int outs = DW ? g.mats : 1, stages = g.terms * g.rsteps * (DW ? 1 : g.mats);
-  const Shape h = DW ? grad_shape(g.n, g.k, outs, stages) : grad_shape(g.k, g.m, outs, stages);
+  const int outs = DW ? g.mats : 1;
+  const Shape h = DW ? grad_shape(g.n, g.k, outs, g.rsteps, g.terms, false) : grad_shape(g.k, g.m, outs, g.rsteps * g.mats, g.terms, true);
   g.splits = h.splits, g.l_blocks = h.l_blocks, g.s_blocks = h.s_blocks;
   g.part = static_cast<float*>(part);
-  const polyq_status r = h.tile == 256 ? run_tile<DW, 2, 4, 4, 2>(g, outs, st)
-                                          : run_tile<DW, 4, 1, 2, 2>(g, outs, st);
+  const polyq_status r = h.tile == 256         ? run_tile<DW, 2, 4, 4, 2, 1>(g, outs, st)
+                         : DW || g.terms == 1 ? run_tile<DW, 4, 1, 2, 2, 1>(g, outs, st)
+                         : g.terms == 2       ? run_tile<DW, 4, 1, 2, 2, DW ? 1 : 2>(g, outs, st)
+                                              : run_tile<DW, 4, 1, 2, 2, DW ? 1 : 3>(g, outs, st);
   if (r != POLYQ_OK || h.splits == 1) return r;
   const int64_t blocks = (static_cast<int64_t>(g.rows) * g.k + 1023) / 1024;
   mx_grad_sum_kernel<<<dim3(static_cast<uint32_t>(blocks), outs), dim3(256), 0, st>>>(g);
@@ -411,11 +421,11 @@ GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int gr
   p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
   p.part_bytes = 0;
   if (dx) {
-    const Shape s = grad_shape(k, m, 1, p.terms * mats * (p.n_pad / kStep));
+    const Shape s = grad_shape(k, m, 1, mats * (p.n_pad / kStep), p.terms, true);
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * m * k * 4);
   }
   if (dw) {
-    const Shape s = grad_shape(n, k, mats, p.terms * (p.m_pad / kStep));
+    const Shape s = grad_shape(n, k, mats, p.m_pad / kStep, p.terms, false);
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * mats * n * k * 4);
   }
   p.total = p.x_bytes + p.plane_bytes + p.xt_bytes + p.part_bytes;
