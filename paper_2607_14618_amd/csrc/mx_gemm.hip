@@ -503,10 +503,6 @@ polyq_status run_gemm(Args a, hipStream_t st) {
   if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
   const size_t lds = 16 * static_cast<size_t>(WM * TM) * kChunkBytes;
   const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM, AHEAD>;
-  if (lds > 65536 &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                          static_cast<int>(lds)) != hipSuccess)
-    return POLYQ_ERR_DEVICE;
   kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(64 * WN * WM), lds, st>>>(a);
   return launched();
 }

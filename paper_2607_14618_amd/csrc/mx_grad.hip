@@ -378,10 +378,6 @@ template <bool DW, int WL, int WS, int TL, int TS, int TERMS>
 polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
   const size_t lds = 2 * static_cast<size_t>(WL * TL * 32) * kStep * 2;
   const auto kernel = mx_grad_kernel<DW, WL, WS, TL, TS, TERMS>;
-  if (lds > 65536 &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                          static_cast<int>(lds)) != hipSuccess)
-    return POLYQ_ERR_DEVICE;
   const int64_t groups = static_cast<int64_t>(g.l_blocks) * g.s_blocks * outs;
   if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
   kernel<<<dim3(static_cast<uint32_t>(groups), g.splits), dim3(64 * WL * WS), lds, st>>>(g);

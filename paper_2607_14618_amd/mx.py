@@ -1,5 +1,6 @@
 """Microscaled 4-bit floating point (MXFP4) on one GPU: quantization, the linear layer,
-the gated feed-forward block and their gradients (marshalling around the C ABI)."""
+the gated feed-forward block and their gradients (marshalling around the C ABI).
+Gradients are computed by the ``_backward`` functions; nothing is recorded for autograd."""
 from __future__ import annotations
 
 import contextlib
@@ -31,6 +32,9 @@ class MXMatrix:
     __slots__ = ("rows", "k", "packed")
 
     def __init__(self, rows: int, k: int, packed: torch.Tensor):
+        nbytes = int(lib().polyq_mx_bytes(rows, k))
+        if nbytes == 0 or packed.dtype != torch.uint8 or not packed.is_contiguous() or packed.numel() < nbytes:
+            raise ValueError(f"a packed matrix of {rows} rows x {k} channels is {nbytes} contiguous bytes (uint8)")
         self.rows, self.k, self.packed = rows, k, packed
 
     @property
@@ -75,7 +79,9 @@ def _empty_matrix(rows: int, k: int, dev: torch.device) -> MXMatrix:
     nbytes = int(lib().polyq_mx_bytes(rows, k))
     if nbytes == 0:
         raise ValueError(f"a matrix of {rows} rows x {k} channels cannot be packed")
-    return MXMatrix(rows, k, _bytes(nbytes, dev))
+    q = MXMatrix.__new__(MXMatrix)
+    q.rows, q.k, q.packed = rows, k, _bytes(nbytes, dev)
+    return q
 
 
 def mx_quantize(x: torch.Tensor) -> MXMatrix:

@@ -113,7 +113,11 @@ def test_binding_refusals():
     with pytest.raises(ValueError, match="act must be"):
         pq.mx_gated(cpu, w, w, act="relu")
     with pytest.raises(ValueError, match="same shape"):
-        pq.mx_gated(cpu, w, pq.MXMatrix(17, 64, w.packed))
+        pq.mx_gated(cpu, w, pq.MXMatrix(15, 64, w.packed))
+    for rows, k, packed in ((17, 64, w.packed), (16, 129, w.packed), (16, 64, w.packed.int()), (16, 64, w.packed[:1279]),
+                            (0, 64, w.packed), (16, 64, torch.zeros((2560,), dtype=torch.uint8)[::2])):
+        with pytest.raises(ValueError, match="packed matrix"):
+            pq.MXMatrix(rows, k, packed)
     with pytest.raises(ValueError, match=r"dh must be"):
         pq.mx_gated_backward(torch.zeros((4, 15)), cpu, w, w)
     with pytest.raises(ValueError, match="dw needs x"):
