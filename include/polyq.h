@@ -499,13 +499,13 @@ polyq_status polyq_mx_unpack(const void* packed, int32_t rows, int32_t k, uint8_
  *   x  [m][k] of x_type, quantized as by polyq_mx_quantize, or a packed matrix [m][k]
  *      (x_type POLYQ_MX_PACKED), which several products can share;
  *   w  packed [n][k];  y  [m][n] of y_type, fully overwritten.
- *   workspace: polyq_mx_workspace_bytes(m, k, x_type) bytes of device scratch, 256-byte
- *   aligned (the packed x; NULL where that is 0); its contents on entry are ignored.
+ *   workspace: polyq_mx_linear_workspace_bytes(m, k, x_type) bytes of device scratch, 256-byte
+ *   aligned (the packed x; none, and NULL, for one or a few tokens and for a packed x); its contents on entry are ignored.
  *   Calls that share one must be ordered.
  * Products of two 4-bit values are exact and summed in fp32; y is rounded once.  Sums
  * are added in a fixed order: the same call gives the same bits.
  */
-size_t polyq_mx_workspace_bytes(int32_t m, int32_t k, int32_t x_type);
+size_t polyq_mx_linear_workspace_bytes(int32_t m, int32_t k, int32_t x_type);
 polyq_status polyq_mx_linear(const void* x, int32_t x_type, int32_t m, const void* w, int32_t n,
                              int32_t k, void* y, int32_t y_type, void* workspace,
                              size_t workspace_bytes, void* stream);
@@ -513,8 +513,10 @@ polyq_status polyq_mx_linear(const void* x, int32_t x_type, int32_t m, const voi
 /*
  * polyq_mx_gated -- the gated feed-forward block's first half in one launch:
  *   h = act(g) u,  g = q(x) G^T,  u = q(x) U^T   (g, u and act in fp32, h rounded once)
- * gate and up packed [n][k], h [m][n] of h_type; x and workspace as for polyq_mx_linear.
+ * gate and up packed [n][k], h [m][n] of h_type; x and workspace as for polyq_mx_linear
+ * (polyq_mx_gated_workspace_bytes).
  */
+size_t polyq_mx_gated_workspace_bytes(int32_t m, int32_t k, int32_t x_type);
 polyq_status polyq_mx_gated(const void* x, int32_t x_type, int32_t m, const void* gate,
                             const void* up, int32_t n, int32_t k, int32_t act, void* h,
                             int32_t h_type, void* workspace, size_t workspace_bytes, void* stream);

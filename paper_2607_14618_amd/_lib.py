@@ -35,7 +35,7 @@ EXPORTS = ("polyq_plan", "polyq_pack", "polyq_pack_rows", "polyq_unpack", "polyq
            "polyq_gemm_batch", "polyq_read_probe", "polyq_gemv_batch_noalloc", "polyq_channel_error",
            "polyq_waterfill", "polyq_quanta_match", "polyq_cluster", "polyq_bit_scaling",
            "polyq_mx_bytes", "polyq_mx_quantize", "polyq_mx_dequantize", "polyq_mx_pack", "polyq_mx_unpack",
-           "polyq_mx_workspace_bytes", "polyq_mx_linear", "polyq_mx_gated",
+           "polyq_mx_linear_workspace_bytes", "polyq_mx_linear", "polyq_mx_gated_workspace_bytes", "polyq_mx_gated",
            "polyq_mx_linear_backward_workspace_bytes", "polyq_mx_linear_backward",
            "polyq_mx_gated_backward_workspace_bytes", "polyq_mx_gated_backward", "polyq_status_str")
 
@@ -142,7 +142,8 @@ def lib() -> ctypes.CDLL:
             L.polyq_mx_dequantize.argtypes = [vp, i32, i32, vp, i32, vp]
             L.polyq_mx_pack.argtypes = [vp, vp, i32, i32, vp, vp]
             L.polyq_mx_unpack.argtypes = [vp, i32, i32, vp, vp, vp]
-            L.polyq_mx_workspace_bytes.argtypes = [i32, i32, i32]
+            L.polyq_mx_linear_workspace_bytes.argtypes = [i32, i32, i32]
+            L.polyq_mx_gated_workspace_bytes.argtypes = [i32, i32, i32]
             L.polyq_mx_linear.argtypes = [vp, i32, i32, vp, i32, i32, vp, i32, vp, sz, vp]
             L.polyq_mx_gated.argtypes = [vp, i32, i32, vp, vp, i32, i32, i32, vp, i32, vp, sz, vp]
             L.polyq_mx_linear_backward_workspace_bytes.argtypes = [i32] * 7
@@ -150,7 +151,8 @@ def lib() -> ctypes.CDLL:
             L.polyq_mx_gated_backward_workspace_bytes.argtypes = [i32] * 7
             L.polyq_mx_gated_backward.argtypes = [vp, i32, vp, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, i32,
                                                   vp, sz, vp]
-            for name in ("polyq_mx_bytes", "polyq_mx_workspace_bytes", "polyq_mx_linear_backward_workspace_bytes",
+            for name in ("polyq_mx_bytes", "polyq_mx_linear_workspace_bytes", "polyq_mx_gated_workspace_bytes",
+                         "polyq_mx_linear_backward_workspace_bytes",
                          "polyq_mx_gated_backward_workspace_bytes"):
                 getattr(L, name).restype = sz
             L.polyq_status_str.argtypes = [ctypes.c_int]

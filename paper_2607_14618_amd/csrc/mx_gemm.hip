@@ -146,13 +146,19 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
     }
     if constexpr (RAW) {  // channels 128 c .. of all tokens, as a record of which N chunks are read
       const int k0 = c * kChunk + lane * 8;
-      for (int t = 0; t < a.m; ++t) {
-        float v[8];
-        load8<T, VEC>(static_cast<const T*>(a.x) + static_cast<int64_t>(t) * a.k, k0, a.k, v);
+      const T* x = static_cast<const T*>(a.x);
+      auto put = [&](int t, const float* v) {
         uint32_t byte;
         const uint32_t code = quantize8(v, &byte);
         *rec.at(t, lane) = code;
         if ((lane & 3) == 0) *rec.scale(t, lane) = static_cast<uint8_t>(byte);
+      };
+      for (int t = 0; t < a.m; t += 2) {  // two tokens' loads at a time
+        float v[2][8];
+        load8<T, VEC>(x + static_cast<int64_t>(t) * a.k, k0, a.k, v[0]);
+        load8<T, VEC>(x + static_cast<int64_t>(min(t + 1, a.m - 1)) * a.k, k0, a.k, v[1]);
+        put(t, v[0]);
+        if (t + 1 < a.m) put(t + 1, v[1]);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       const uint32_t word = reinterpret_cast<const uint32_t*>(rec.scales)[lane];
@@ -575,8 +581,14 @@ polyq_status launch_gated_grad(const void* gate, const void* up, const void* x, 
 
 namespace {
 
-// Up to this many tokens every work-group quantizes the activations itself.
-constexpr int kRawTokens = 4;
+// Up to this many tokens every work-group quantizes the activations itself; more are quantized once, in a launch before.
+// Itself / once, us for 1, 2, 3, 4 and 8 tokens: linear 5120 x 5120 5.9 6.4 7.4 8.1 11.3 / 8.1 8.3 8.4 8.5 8.6, of 5120 x
+// 13824 12.5 12.4 14.5 15.6 22.1 / 16.9 15.8 15.9 16.2 16.2; gated 13824 x 5120 18.3 18.6 21.3 22.5 28.9 / 20.6 20.3
+// 20.4 20.8 21.0, of 25600 x 5120 30.4 29.5 35.0 36.1 47.0 / 33.8 30.7 31.1 31.5 32.0.
+constexpr int raw_tokens(bool gated) { return gated ? 2 : 4; }
+size_t product_bytes(int32_t m, int32_t k, int x_type, bool gated) {
+  return float_type(x_type) && m > raw_tokens(gated) ? polyq_mx_bytes(m, k) : 0;
+}
 
 polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const void* w1, int32_t n, int32_t k, int act,
                      void* y, int y_type, void* ws, size_t ws_bytes, hipStream_t st) {
@@ -586,7 +598,7 @@ polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const
   if (!valid_shape(m, k) || !valid_shape(n, k)) return POLYQ_ERR_SHAPE;
   if (!aligned(w0, 256) || !aligned(w1, 256) || !aligned(y, type_bytes(y_type))) return POLYQ_ERR_ARG;
   if (!aligned(x, x_type == POLYQ_MX_PACKED ? 256 : type_bytes(x_type))) return POLYQ_ERR_ARG;
-  const size_t need = polyq_mx_workspace_bytes(m, k, x_type);
+  const size_t need = product_bytes(m, k, x_type, act >= 0);
   if (need > 0 && (ws == nullptr || ws_bytes < need)) return POLYQ_ERR_CAPACITY;
   if (need > 0 && !aligned(ws, 256)) return POLYQ_ERR_ARG;
   Args a{};
@@ -611,8 +623,11 @@ polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const
 
 using namespace polyq;
 
-extern "C" size_t polyq_mx_workspace_bytes(int32_t m, int32_t k, int32_t x_type) {
-  return mx::float_type(x_type) && m > mx::kRawTokens ? polyq_mx_bytes(m, k) : 0;
+extern "C" size_t polyq_mx_linear_workspace_bytes(int32_t m, int32_t k, int32_t x_type) {
+  return mx::product_bytes(m, k, x_type, false);
+}
+extern "C" size_t polyq_mx_gated_workspace_bytes(int32_t m, int32_t k, int32_t x_type) {
+  return mx::product_bytes(m, k, x_type, true);
 }
 
 extern "C" polyq_status polyq_mx_linear(const void* x, int32_t x_type, int32_t m, const void* w, int32_t n, int32_t k,

@@ -180,7 +180,8 @@ def _product(name: str, x: Activations, ws, act: Optional[str], dtype, y, worksp
     ot = _type(dtype, "the output")
     y = _output(y, (m, ws[0].rows), dtype, dev, "the output")
     L = lib()
-    need = 0 if t == PACKED else int(L.polyq_mx_workspace_bytes(m, ws[0].k, t))
+    size = L.polyq_mx_linear_workspace_bytes if act is None else L.polyq_mx_gated_workspace_bytes
+    need = 0 if t == PACKED else int(size(m, ws[0].k, t))
     ptr, nbytes, _keep = _scratch(workspace, need, dev)
     n, k = ws[0].shape
     with _on(dev):

@@ -154,7 +154,7 @@ def test_quantize_reads_unaligned_rows():
 
 
 # ------------------------------------------------------------------ linear, gated
-SHAPES = [(1, 1, 1), (1, 16, 128), (2, 17, 129), (1, 100, 5120), (16, 130, 640), (5, 64, 2976), (17, 33, 515),
+SHAPES = [(1, 1, 1), (1, 16, 128), (2, 40, 1111), (3, 100, 700), (4, 33, 2049), (2, 17, 129), (1, 100, 5120), (16, 130, 640), (5, 64, 2976), (17, 33, 515),
           (33, 1357, 513), (77, 200, 2976), (64, 256, 1024), (130, 300, 384), (257, 129, 640), (16, 5120, 160)]
 
 
@@ -269,7 +269,7 @@ def act_tol(g, a):
 
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("t", list(F))
-@pytest.mark.parametrize("m,n,k", [(1, 16, 128), (1, 1, 3), (3, 100, 5120), (16, 130, 640), (33, 77, 515),
+@pytest.mark.parametrize("m,n,k", [(1, 16, 128), (1, 1, 3), (2, 20, 2050), (3, 100, 5120), (16, 130, 640), (33, 77, 515),
                                    (130, 300, 384), (257, 129, 640)])
 def test_gated(m, n, k, t, act):
     x, gate, up = activations(m, k, t, m + n), weights(n, k, 1), weights(n, k, 2)

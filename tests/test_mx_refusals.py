@@ -25,8 +25,11 @@ def test_sizes():
     assert call("polyq_mx_bytes", 5120, 13824) == 320 * (27 * 4352)
     for rows, k in ((0, 1), (1, 0), (-1, 5), (5, -1), ((1 << 24) + 1, 8), (1, (1 << 20) + 1)):
         assert call("polyq_mx_bytes", rows, k) == 0
-    assert call("polyq_mx_workspace_bytes", 17, 513, 2) == call("polyq_mx_bytes", 17, 513)
-    assert call("polyq_mx_workspace_bytes", 17, 513, 3) == 0
+    for op in ("linear", "gated"):
+        assert call(f"polyq_mx_{op}_workspace_bytes", 17, 513, 2) == call("polyq_mx_bytes", 17, 513)
+        assert call(f"polyq_mx_{op}_workspace_bytes", 17, 513, 3) == 0
+        assert call(f"polyq_mx_{op}_workspace_bytes", 1, 513, 0) == 0
+        assert call(f"polyq_mx_{op}_workspace_bytes", 0, 513, 0) == 0
     assert call("polyq_mx_linear_backward_workspace_bytes", 0, 1, 1, 0, 0, 1, 1) == 0
     assert call("polyq_mx_gated_backward_workspace_bytes", 1, 1, 1, 0, 7, 1, 1) == 0
     assert call("polyq_mx_bytes", 1 << 24, 1 << 20) > 1 << 43     # no overflow
