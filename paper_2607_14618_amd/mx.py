@@ -3,7 +3,6 @@ the gated feed-forward block and their gradients (marshalling around the C ABI).
 Gradients are computed by the ``_backward`` functions; nothing is recorded for autograd."""
 from __future__ import annotations
 
-import contextlib
 from typing import Optional, Tuple, Union
 
 import torch
@@ -17,12 +16,25 @@ PACKED = 3
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 
-# The current stream's handle without a Stream object around it (0.2 us of a call's 8 instead of 2).
+# torch's own lookups of the current stream and device build objects around them (2 us of a call's 7).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(dev: torch.device) -> int:
     return _lib._stream(dev) if _raw_stream is None else _raw_stream(dev.index)
+
+
+def _launch(name: str, dev: torch.device, *args) -> None:
+    """Calls the library on the tensors' device, whatever the current one is, and its current stream."""
+    fn = getattr(lib(), name)
+    if dev.index == _current():
+        status = fn(*args, _stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _stream(dev))
+    if status != 0:
+        _check(status, name)
 
 
 class MXMatrix:
@@ -47,14 +59,6 @@ class MXMatrix:
 
     def __repr__(self):
         return f"MXMatrix(rows={self.rows}, k={self.k}, device={self.device})"
-
-
-_HERE = contextlib.nullcontext()
-
-
-def _on(dev: torch.device):
-    """Launches go to the tensors' device, whatever the current one is."""
-    return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
 
 def _bytes(nbytes: int, dev: torch.device) -> torch.Tensor:
@@ -90,9 +94,7 @@ def mx_quantize(x: torch.Tensor) -> MXMatrix:
     x2 = _two(x, "x")
     dev = _need_cuda(x2)
     out = _empty_matrix(x2.shape[0], x2.shape[1], dev)
-    with _on(dev):
-        _check(lib().polyq_mx_quantize(_ptr(x2), t, out.rows, out.k, _ptr(out.packed), _stream(dev)),
-               "polyq_mx_quantize")
+    _launch("polyq_mx_quantize", dev, x2.data_ptr(), t, out.rows, out.k, out.packed.data_ptr())
     return out
 
 
@@ -101,9 +103,7 @@ def mx_dequantize(q: MXMatrix, dtype: torch.dtype = torch.float32) -> torch.Tens
     t = _type(dtype, "dtype")
     dev = _need_cuda(q.packed)
     out = torch.empty((q.rows, q.k), dtype=dtype, device=dev)
-    with _on(dev):
-        _check(lib().polyq_mx_dequantize(_ptr(q.packed), q.rows, q.k, _ptr(out), t, _stream(dev)),
-               "polyq_mx_dequantize")
+    _launch("polyq_mx_dequantize", dev, q.packed.data_ptr(), q.rows, q.k, out.data_ptr(), t)
     return out
 
 
@@ -118,9 +118,7 @@ def mx_pack(codes: torch.Tensor, scales: torch.Tensor, k: int) -> MXMatrix:
     if tuple(scales.shape) != (codes.shape[0], -(-k // BLOCK)):
         raise ValueError(f"scales shape {tuple(scales.shape)} is not [{codes.shape[0]}][{-(-k // BLOCK)}]")
     out = _empty_matrix(codes.shape[0], int(k), dev)
-    with _on(dev):
-        _check(lib().polyq_mx_pack(_ptr(codes), _ptr(scales), out.rows, out.k, _ptr(out.packed), _stream(dev)),
-               "polyq_mx_pack")
+    _launch("polyq_mx_pack", dev, _ptr(codes), _ptr(scales), out.rows, out.k, _ptr(out.packed))
     return out
 
 
@@ -129,9 +127,7 @@ def mx_unpack(q: MXMatrix) -> Tuple[torch.Tensor, torch.Tensor]:
     dev = _need_cuda(q.packed)
     codes = torch.empty((q.rows, (q.k + 1) // 2), dtype=torch.uint8, device=dev)
     scales = torch.empty((q.rows, -(-q.k // BLOCK)), dtype=torch.uint8, device=dev)
-    with _on(dev):
-        _check(lib().polyq_mx_unpack(_ptr(q.packed), q.rows, q.k, _ptr(codes), _ptr(scales), _stream(dev)),
-               "polyq_mx_unpack")
+    _launch("polyq_mx_unpack", dev, _ptr(q.packed), q.rows, q.k, _ptr(codes), _ptr(scales))
     return codes, scales
 
 
@@ -173,24 +169,26 @@ def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev: torch.device):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
-def _product(name: str, x: Activations, ws, act: Optional[str], dtype, y, workspace):
+def _product(x: Activations, ws, act: Optional[int], dtype, y, workspace):
     held, t, m, out = _input(x, *ws)
-    dev = _need_cuda(held, y, workspace, *(w.packed for w in ws))
+    w = ws[0]
+    dev = _need_cuda(held, y, workspace, *[v.packed for v in ws])
     dtype = y.dtype if dtype is None and y is not None else out if dtype is None else dtype
     ot = _type(dtype, "the output")
-    y = _output(y, (m, ws[0].rows), dtype, dev, "the output")
-    L = lib()
-    size = L.polyq_mx_linear_workspace_bytes if act is None else L.polyq_mx_gated_workspace_bytes
-    need = 0 if t == PACKED else int(size(m, ws[0].k, t))
+    y = _output(y, (m, w.rows), dtype, dev, "the output")
+    if t == PACKED:
+        need = 0
+    elif act is None:
+        need = lib().polyq_mx_linear_workspace_bytes(m, w.k, t)
+    else:
+        need = lib().polyq_mx_gated_workspace_bytes(m, w.k, t)
     ptr, nbytes, _keep = _scratch(workspace, need, dev)
-    n, k = ws[0].shape
-    with _on(dev):
-        if act is None:
-            st = L.polyq_mx_linear(_ptr(held), t, m, _ptr(ws[0].packed), n, k, _ptr(y), ot, ptr, nbytes, _stream(dev))
-        else:
-            st = L.polyq_mx_gated(_ptr(held), t, m, _ptr(ws[0].packed), _ptr(ws[1].packed), n, k, ACTIVATIONS[act],
-                                  _ptr(y), ot, ptr, nbytes, _stream(dev))
-    _check(st, name)
+    if act is None:
+        _launch("polyq_mx_linear", dev, held.data_ptr(), t, m, w.packed.data_ptr(), w.rows, w.k, y.data_ptr(), ot, ptr,
+                nbytes)
+    else:
+        _launch("polyq_mx_gated", dev, held.data_ptr(), t, m, w.packed.data_ptr(), ws[1].packed.data_ptr(), w.rows, w.k,
+                act, y.data_ptr(), ot, ptr, nbytes)
     return y
 
 
@@ -199,15 +197,14 @@ def mx_linear(x: Activations, w: MXMatrix, dtype: Optional[torch.dtype] = None, 
     """y [m][n] = q(x) W^T, q(x) the microscaled 4-bit form of x.  x is [m][k] (fp32,
     fp16 or bf16; one row as [k]) or a packed matrix, which several products can share;
     y has x's type (bf16 for a packed x) unless ``dtype`` or ``y`` says otherwise."""
-    return _product("polyq_mx_linear", x, (w,), None, dtype, y, workspace)
+    return _product(x, (w,), None, dtype, y, workspace)
 
 
 def mx_gated(x: Activations, gate: MXMatrix, up: MXMatrix, act: str = "silu", dtype: Optional[torch.dtype] = None,
              y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """h [m][n] = act(q(x) gate^T) * (q(x) up^T) in one launch; act: "silu", "gelu" or
     "gelu_tanh".  x, dtype and y as for ``mx_linear``."""
-    _act(act)
-    return _product("polyq_mx_gated", x, (gate, up), act, dtype, y, workspace)
+    return _product(x, (gate, up), _act(act), dtype, y, workspace)
 
 
 def _act(act: str) -> int:
@@ -245,12 +242,10 @@ def mx_linear_backward(dy: torch.Tensor, x: Optional[Activations], w: MXMatrix, 
     gt = _type(dtype, "dtype")
     dx = torch.empty((m, w.k), dtype=dtype, device=dev) if need_dx else None
     dw = torch.empty((w.rows, w.k), dtype=dtype, device=dev) if need_dw else None
-    L = lib()
-    need = int(L.polyq_mx_linear_backward_workspace_bytes(m, w.rows, w.k, t, gt, need_dx, need_dw))
+    need = int(lib().polyq_mx_linear_backward_workspace_bytes(m, w.rows, w.k, t, gt, need_dx, need_dw))
     ptr, nbytes, _keep = _scratch(workspace, need, dev)
-    with _on(dev):
-        _check(L.polyq_mx_linear_backward(_ptr(d), dt, _ptr(held), t, m, _ptr(w.packed), w.rows, w.k, _ptr(dx), _ptr(dw),
-                                          gt, ptr, nbytes, _stream(dev)), "polyq_mx_linear_backward")
+    _launch("polyq_mx_linear_backward", dev, _ptr(d), dt, _ptr(held), t, m, _ptr(w.packed), w.rows, w.k, _ptr(dx), _ptr(dw),
+            gt, ptr, nbytes)
     return dx, dw
 
 
@@ -271,11 +266,8 @@ def mx_gated_backward(dh: torch.Tensor, x: Activations, gate: MXMatrix, up: MXMa
     gt = _type(dtype, "dtype")
     dx = torch.empty((m, k), dtype=dtype, device=dev) if need_dx else None
     dg, du = (torch.empty((n, k), dtype=dtype, device=dev) if need_dw else None for _ in range(2))
-    L = lib()
-    need = int(L.polyq_mx_gated_backward_workspace_bytes(m, n, k, t, gt, need_dx, need_dw))
+    need = int(lib().polyq_mx_gated_backward_workspace_bytes(m, n, k, t, gt, need_dx, need_dw))
     ptr, nbytes, _keep = _scratch(workspace, need, dev)
-    with _on(dev):
-        _check(L.polyq_mx_gated_backward(_ptr(d), dt, _ptr(held), t, m, _ptr(gate.packed), _ptr(up.packed), n, k, a,
-                                         _ptr(dx), _ptr(dg), _ptr(du), gt, ptr, nbytes, _stream(dev)),
-               "polyq_mx_gated_backward")
+    _launch("polyq_mx_gated_backward", dev, _ptr(d), dt, _ptr(held), t, m, _ptr(gate.packed), _ptr(up.packed), n, k, a,
+            _ptr(dx), _ptr(dg), _ptr(du), gt, ptr, nbytes)
     return dx, dg, du
