@@ -274,16 +274,16 @@ __device__ __forceinline__ int64_t plane_at(int row, int col, int cols_pad) {
   return (static_cast<int64_t>(row >> 5) * (cols_pad >> 4) + (col >> 4)) * 1024 + (row & 31) * 32 + (col & 15) * 2;
 }
 
-// Two transposing LDS reads: lane j of 16 gets column j of the rows those 16 lanes address (8 bytes each, four
-// lanes a row), and of the four rows `next` bytes further on.
-__device__ __forceinline__ bf16x8 read_transposed(const uint8_t* p, int next = 128) {
+// Two transposing LDS reads: lane j of 16 gets column j of the four rows those 16 lanes address with p (8 bytes each,
+// four lanes a row), and of the four they address with q.
+__device__ __forceinline__ bf16x8 read_transposed(const uint8_t* p, const uint8_t* q) {
   typedef short s4 __attribute__((ext_vector_type(4)));
   union {
     s4 h[2];
     bf16x8 v;
   } u;
   u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(p));
-  u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(p + next));
+  u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(q));
   return u.v;
 }
 
@@ -311,7 +311,8 @@ __device__ __forceinline__ void transpose_chunk(uint8_t* lds, i4v codes, uint32_
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int ct = chunk * 4 + q;
-    const bf16x8 v = read_transposed(lds + q * kBlockBytes + (upper * 8 + (i >> 2)) * 64 + half * 32 + (i & 3) * 8, 4 * 64);
+    const uint8_t* p = lds + q * kBlockBytes + (upper * 8 + (i >> 2)) * 64 + half * 32 + (i & 3) * 8;
+    const bf16x8 v = read_transposed(p, p + 4 * 64);
     if (ct < c_tiles)
       *reinterpret_cast<bf16x8*>(out + (static_cast<int64_t>(ct) * m_tiles + tile) * kBlockBytes + (half * 16 + i) * 32 + upper * 16) = v;
   }

@@ -22,7 +22,10 @@ namespace {
 // A gradient product of either kind is D[l][s] = sum_r L[r][l] S[s][r]:
 //   dx   l = c, s = t, r = n:  L = W, converted;           S = d
 //   dW   l = n, s = c, r = t:  L = d;                      S = x^ transposed, converted once
-// L passes through LDS in blocks of 32 r x 16 l (1 KiB, rows of 32 bytes) and is read transposed;
+// L passes through LDS in blocks of 32 r x 16 l (1 KiB, rows of 32 bytes) and is read transposed; in blocks of odd l
+// tiles rows 4 .. 7 change places with 0 .. 3 (and 12 .. 15 with 8 .. 11), so that a fragment's two
+// tiles are read from different banks, and dx's converted rows 8 .. 15 have their 16-byte halves
+// exchanged, so that they are written to other banks than 0 .. 7;
 // S is stored in memory as blocks of 32 s x 16 r, which are the operand fragments of a
 // wave, and goes from there into registers.
 constexpr int kStep = 64;            // r of a stage
@@ -115,7 +118,7 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
   auto store_blocks = [&](int half) {
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i)
-      *reinterpret_cast<i4v*>(lds + half * STAGE + (i * W + wave) * kBlockBytes + lane * 16) = blocks[i];
+      *reinterpret_cast<i4v*>(lds + half * STAGE + (i * W + wave) * kBlockBytes + ((lane * 16) ^ ((wave & 1) * 128))) = blocks[i];
   };
   // L of dx: packed fragments (16 r x 128 l) into registers, and from there as bf16 into LDS.
   const int chunks = chunks_of(g.k), b_tiles = tiles_of(g.n);
@@ -153,19 +156,22 @@ __global__ __launch_bounds__(64 * WL * WS, 2) void mx_grad_kernel(const GradArgs
         v[w * 4 + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3));
       }
       const int lt = f / (kStep / kRows) * 8 + (lane >> 4) * 2 + H;
-      uint8_t* dst = lds + half * STAGE + ((rt >> 1) * (L / 16) + lt) * kBlockBytes + ((rt & 1) * 16 + (lane & 15)) * 32;
-      *reinterpret_cast<u4v*>(dst) = u4v{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<u4v*>(dst + 16) = u4v{v[4], v[5], v[6], v[7]};
+      uint8_t* dst = lds + half * STAGE + ((rt >> 1) * (L / 16) + lt) * kBlockBytes + ((rt & 1) * 16 + ((lane & 15) ^ (H * 4))) * 32;
+      const int first = ((lane >> 3) & 1) * 16;
+      *reinterpret_cast<u4v*>(dst + first) = u4v{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<u4v*>(dst + (first ^ 16)) = u4v{v[4], v[5], v[6], v[7]};
     }
   };
   // Fragment of 32 l x 16 r: a transposing read hands lane j of 16 lanes column j of the four rows whose 32
   // bytes those lanes address; lane groups 1 and 3 have l 16 .. 31, groups 2 and 3 r 8 .. 15.
-  const int l_lane = ((lane >> 4) & 1) * kBlockBytes + ((lane >> 5) * 8 + ((lane & 15) >> 2)) * 32 + (lane & 3) * 8;
+  const int odd = (lane >> 4) & 1;
+  const int l_lane = odd * kBlockBytes + ((lane >> 5) * 8 + ((lane & 15) >> 2)) * 32 + (((lane & 3) * 8) ^ (DW ? 0 : (lane >> 5) * 16));
+  const int l_first = l_lane + odd * 128, l_second = l_lane + (odd ^ 1) * 128;
   bf16x8 lf[2][TL];
   auto read_l = [&](int half, int step, int to) {
-    const uint8_t* base = lds + half * STAGE + ((step >> 1) * (L / 16) + wl * TL * 2) * kBlockBytes + (step & 1) * 512 + l_lane;
+    const uint8_t* base = lds + half * STAGE + ((step >> 1) * (L / 16) + wl * TL * 2) * kBlockBytes + (step & 1) * 512;
 #pragma unroll
-    for (int i = 0; i < TL; ++i) lf[to][i] = read_transposed(base + i * 2 * kBlockBytes);
+    for (int i = 0; i < TL; ++i) lf[to][i] = read_transposed(base + l_first + i * 2 * kBlockBytes, base + l_second + i * 2 * kBlockBytes);
   };
 
   f16v acc[TL][TS];
