@@ -1,4 +1,5 @@
-"""MI355X (gfx950) mixed-bit linear layer: PolyQ's decode GEMV and prefill GEMM.
+"""MI355X (gfx950) mixed-bit linear layer: PolyQ's decode GEMV and prefill GEMM; and linear layers, the gated
+block and their gradients in microscaled 4-bit floating point (mx_*).
 
 Python binding of libpolyq.so (include/polyq.h).  The functions take torch
 tensors for device memory and run on torch's current HIP stream.

@@ -1,6 +1,11 @@
 // Products of microscaled 4-bit matrices: the linear layer y = x^ W^T and the gated block
 // h = act(x^ G^T) * (x^ U^T), x^ the quantized activations; and the gated block's
 // g, u once more in its backward pass, where dg and du leave instead of h.
+//
+// x^ and the weights are multiplied in their 4 bits: a lane's 16 bytes and scale byte of the packed layout are what it
+// hands to a scaled matrix instruction, so nothing is unpacked.  Three kernels: up to 16 tokens read every weight once and
+// are bound by that (mx_stream_kernel), some tokens by latency (mx_split_kernel), many by the matrix cores
+// (mx_gemm_kernel); choose() says which.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -99,6 +104,10 @@ __device__ __forceinline__ void finish_pair(const Args& a, int token, int n0, in
 // token tile; its waves split K and their sums meet in LDS.  T: the activations' type, which
 // every wave then quantizes for its own part of K in its own LDS (one launch instead of
 // two); or `Packed`.
+// What bounds it: memory.  Gate and up of 13824 x 5120, one token: 75 MB in 13 to 15 us (5.0 to 5.7 TB/s), of 25600 x 5120, 16
+// tokens: 139 MB in 28 us (5.0 TB/s); 5120 x 5120, one token: 5.6 us, of which a launch is 2.  Eight waves share K so that a
+// few hundred work-groups have all weights in flight: with 4 waves 14.1 us in place of 15.3 and 29.3 in place of 28.4, with
+// 16 20.2 and 31.9; two row tiles of each matrix a work-group 16.2 and 33.8.
 struct Packed {};
 template <int MODE, class T, bool VEC, int TN, int W>
 __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
@@ -206,7 +215,8 @@ __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {
 // ---------------------------------------------------------------- some tokens
 // A work-group of W waves takes 32 rows (of each matrix) by TM x 32 tokens, its waves split K, and
 // their sums meet in LDS: many work-groups where the outputs are few.  Both operands
-// come straight from memory, the tokens from L2.
+// come straight from memory, the tokens from L2.  77 tokens, 1357 x 2976: 4.7 us, where the tiled kernel below walks all of
+// K in one work-group and takes 9.7.
 template <int MODE, int TM, int W>
 __global__ __launch_bounds__(64 * W, 2) void mx_split_kernel(const Args a) {
   constexpr int NM = MODE == kLinear ? 1 : 2;
@@ -300,8 +310,16 @@ __global__ __launch_bounds__(64 * W, 2) void mx_split_kernel(const Args a) {
 // WN x WM waves, each TN x 32 rows (the gated modes: TN / 2 x 32 of each matrix) by TM x 32
 // tokens.  K is walked a record (4 chunks) at a time.  The tokens' fragments go from
 // memory straight into one half of a ring in LDS while the other half is multiplied; the
-// weights' fragments are what their wave alone multiplies and go into its registers,
-// two chunks ahead.
+// weights' fragments are what their wave alone multiplies and go into its registers, AHEAD
+// chunks ahead.  Through LDS both operands of such a tile would ask for 94 of its 128 bytes a
+// clock; so it is 64 there and 48 of 64 from the caches.  Fragments are read half a chunk ahead
+// of their products, in the order written (the scheduler would sink them to their uses).
+// What bounds it: the matrix cores and what their power leaves.  On random values a loop of nothing but these
+// instructions reaches 6.5 to 7.0 PFLOP/s (clocks fall to 2.0 GHz), gate/up of 2000 tokens x 13824 x 5120 3.7 (153 us, of
+// which 1728 work-groups in rounds of 512 leave a sixth idle, loads cost 20 and the epilogue 30), the down projection
+// 3.4 (82 us).  Measured on the way for the former: 16x16x128 instructions and both operands in LDS 228 us, weights in
+// registers 205, 32x32x64 instructions and buffer loads into LDS (after the global form the compiler waits for all loads)
+// 176, activations by hardware exp2 and reciprocal 157, 16-byte stores 153.  One wave per SIMD with twice the tile: 247.
 template <int MODE, int WN, int WM, int TN, int TM, int AHEAD>
 __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) {
   constexpr int W = WN * WM, CT = WM * TM;

@@ -27,7 +27,16 @@ namespace {
 // tiles are read from different banks, and dx's converted rows 8 .. 15 have their 16-byte halves
 // exchanged, so that they are written to other banks than 0 .. 7;
 // S is stored in memory as blocks of 32 s x 16 r, which are the operand fragments of a
-// wave, and goes from there into registers.
+// wave, and goes from there into registers a stage ahead.
+// A stage is 64 r: four steps of products, each wave reading the next step's L ahead of them and converting the next
+// stage's W between them; one barrier a stage.
+// What bounds it: the matrix cores (2.0 PFLOP/s of nothing but these instructions on random values) at the share that whole
+// tiles leave of a round: 2000 tokens, 5120 x 13824: dx 256 us (1106 TFLOP/s; 432 tiles on 256 compute units), dW 265 (1068;
+// 1080 tiles); gated 13824 x 5120: dx 485 + 23 for the sum of 3 splits (1167), dW 495 (1144).  A library product of the same
+// bf16 shapes reaches 950 to 1250.  Tried: 128 x 128 a wave, one wave per SIMD (312, 318 us for the first two); 128 x 256 and 256
+// x 128 by four waves, two work-groups a compute unit (290, 290); work-groups that walk several outputs with the next one's
+// loads under way (280, 290); L of dW by loads straight into LDS, for which the compiler waits before every transposing
+// read (282, 316).
 constexpr int kStep = 64;            // r of a stage
 constexpr int kMaxRows = 1 << 21;    // tokens and output channels: a work-group's S is reached with 32-bit offsets
 

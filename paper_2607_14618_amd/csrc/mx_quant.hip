@@ -12,6 +12,9 @@
 // takes one record, 16 rows x 512 values, a wave four of its rows: the 64 lanes read 8
 // values each of a row (1 or 2 KiB in a row), form the block's maximum over 4 lanes and
 // convert; the codes meet in LDS, from where they leave as whole 1 KiB fragments.
+// 4096 x 13824 bf16: 27.5 us (143 MB, 5.2 TB/s), back 22.2 us; 2000 x 13824 15.5, with the transposed blocks in
+// place of the packed form 26 (111 MB).  One token 3.1 us.  A wave per record, its 16 rows one
+// after the other, took 33, 21 and 5.4.
 #include <hip/hip_runtime.h>
 
 #include "mx.h"
