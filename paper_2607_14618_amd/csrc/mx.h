@@ -26,11 +26,8 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
 __host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
 __host__ __device__ inline int chunks_of(int k) { return div_up(k, kChunk); }
@@ -147,9 +144,6 @@ struct BF16 { typedef __bf16 type; };
 
 inline bool float_type(int t) { return t == POLYQ_MX_F32 || t == POLYQ_MX_F16 || t == POLYQ_MX_BF16; }
 inline int type_bytes(int t) { return t == POLYQ_MX_F32 ? 4 : 2; }
-
-template <class T>
-__device__ __forceinline__ float load1(const T* p) { return static_cast<float>(*p); }
 
 // Four consecutive elements; vec: p is aligned to all four.
 template <class T>
@@ -368,6 +362,7 @@ inline bool valid_act(int act) { return act == POLYQ_ACT_SILU || act == POLYQ_AC
 inline bool valid_shape(int32_t rows, int32_t k) {
   return rows >= 1 && rows <= POLYQ_MAX_N && k >= 1 && k <= POLYQ_MAX_K;
 }
+inline polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // x [rows][k] into the packed layout and, if asked for, into transposed blocks (transpose_chunk; rows padded to 64);

@@ -496,8 +496,6 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) 
 }
 
 // ---------------------------------------------------------------- launches
-polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
-
 template <int MODE, class T, bool VEC>
 polyq_status run_stream(const Args& a, hipStream_t st) {
   constexpr int TN = MODE == kLinear ? 1 : 2, W = 8;

@@ -360,26 +360,25 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const void* __restrict__
     *reinterpret_cast<bf16x4*>(planes + t * (static_cast<int64_t>(m_pad) * n_pad * 2) + plane_at(row, col, n_pad)) = next_terms(&v);
 }
 
-polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
-
 inline int64_t pad64(int64_t v) { return align_up(v, 64); }
 
-// One gradient product's tile and splits: outputs of `l` by `s`, `stages` of the reduction.
+// One gradient product's tile (l x s) and splits: 256 x 256 by eight waves where that makes 128 tiles, or 256 x 64 by four;
+// of dx, whose small tiles take all terms in one stage, 128 x 64 where those are few, which makes the stages
+// shorter and more of them at once.  256 x 64 / 128 x 64, dx with its sums (us): 64 tokens, 1024 x 5120 fp32 26.3 / 17.7, 5120 x
+// 5120 bf16 24.3 / 23.6; 500 tokens, 5120 x 13824 102 / 110.
+// The reduction (`steps` stages of each of `terms`) is split where rounds of whole tiles leave much of the GPU idle; a split
+// costs its partial sums, about as much as 8 stages, and has at least 8.
 struct Shape {
-  int tile;  // 256 x 256 of l x s by eight waves, or 256 x 64 by four
-  int l_blocks, s_blocks, splits;
+  int l, s, l_blocks, s_blocks, splits;
 };
-// `steps` stages of each of `terms`; `shared`: the small tile takes all terms in one stage.
-Shape grad_shape(int l, int s, int outs, int steps, int terms, bool shared) {
+Shape grad_shape(bool dw, int l, int s, int outs, int steps, int terms) {
   Shape h;
-  const int64_t big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs;
-  h.tile = big < 128 ? 64 : 256;
-  h.l_blocks = div_up(l, 256), h.s_blocks = div_up(s, h.tile);
+  const bool big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs >= 128;
+  const bool few = !dw && static_cast<int64_t>(div_up(l, 256)) * div_up(s, 64) <= 64;
+  h.l = few ? 128 : 256, h.s = big ? 256 : 64;
+  h.l_blocks = div_up(l, h.l), h.s_blocks = div_up(s, h.s);
   const int64_t groups = static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs;
-  const int stages = shared && h.tile == 64 ? steps : steps * terms;
-  // Work-groups that run at once: one or two per compute unit.  The reduction is split where rounds of whole tiles
-  // leave much of the GPU idle; a split costs its partial sums, about as much as 8 stages, and has at least 8.
-  const int slots = h.tile == 256 ? kCUs : 2 * kCUs;
+  const int stages = dw || big ? steps * terms : steps, slots = big ? kCUs : few ? 4 * kCUs : 2 * kCUs;  // slots: work-groups at once
   h.splits = 1;
   int64_t best = -1;
   for (int n = 1; n <= 32 && (n == 1 || stages / n >= 8); ++n) {
@@ -402,13 +401,20 @@ polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
 template <bool DW>
 polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
   const int outs = DW ? g.mats : 1;
-  const Shape h = DW ? grad_shape(g.n, g.k, outs, g.rsteps, g.terms, false) : grad_shape(g.k, g.m, outs, g.rsteps * g.mats, g.terms, true);
+  const Shape h = DW ? grad_shape(true, g.n, g.k, outs, g.rsteps, g.terms) : grad_shape(false, g.k, g.m, 1, g.rsteps * g.mats, g.terms);
   g.splits = h.splits, g.l_blocks = h.l_blocks, g.s_blocks = h.s_blocks;
   g.part = static_cast<float*>(part);
-  const polyq_status r = h.tile == 256         ? run_tile<DW, 2, 4, 4, 2, 1>(g, outs, st)
-                         : DW || g.terms == 1 ? run_tile<DW, 4, 1, 2, 2, 1>(g, outs, st)
-                         : g.terms == 2       ? run_tile<DW, 4, 1, 2, 2, DW ? 1 : 2>(g, outs, st)
-                                              : run_tile<DW, 4, 1, 2, 2, DW ? 1 : 3>(g, outs, st);
+  polyq_status r;
+  if (h.s == 256) r = run_tile<DW, 2, 4, 4, 2, 1>(g, outs, st);
+  else if constexpr (DW) r = run_tile<true, 4, 1, 2, 2, 1>(g, outs, st);
+  else if (h.l == 256)
+    r = g.terms == 1   ? run_tile<false, 4, 1, 2, 2, 1>(g, 1, st)
+        : g.terms == 2 ? run_tile<false, 4, 1, 2, 2, 2>(g, 1, st)
+                       : run_tile<false, 4, 1, 2, 2, 3>(g, 1, st);
+  else
+    r = g.terms == 1   ? run_tile<false, 2, 2, 2, 1, 1>(g, 1, st)
+        : g.terms == 2 ? run_tile<false, 2, 2, 2, 1, 2>(g, 1, st)
+                       : run_tile<false, 2, 2, 2, 1, 3>(g, 1, st);
   if (r != POLYQ_OK || h.splits == 1) return r;
   const int64_t blocks = (static_cast<int64_t>(g.rows) * g.k + 1023) / 1024;
   mx_grad_sum_kernel<<<dim3(static_cast<uint32_t>(blocks), outs), dim3(256), 0, st>>>(g);
@@ -432,11 +438,11 @@ GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int gr
   p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
   p.part_bytes = 0;
   if (dx) {
-    const Shape s = grad_shape(k, m, 1, mats * (p.n_pad / kStep), p.terms, true);
+    const Shape s = grad_shape(false, k, m, 1, mats * (p.n_pad / kStep), p.terms);
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * m * k * 4);
   }
   if (dw) {
-    const Shape s = grad_shape(n, k, mats, p.m_pad / kStep, p.terms, false);
+    const Shape s = grad_shape(true, n, k, mats, p.m_pad / kStep, p.terms);
     if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * mats * n * k * 4);
   }
   p.total = p.x_bytes + p.plane_bytes + p.xt_bytes + p.part_bytes;

@@ -170,8 +170,6 @@ __global__ __launch_bounds__(256) void mx_repack_kernel(const uint8_t* __restric
 // rows and k as they have to be, the work-groups of a launch over `jobs` within the grid's limit
 polyq_status check_jobs(int64_t groups) { return groups > 0x7FFFFFFFll ? POLYQ_ERR_CAPACITY : POLYQ_OK; }
 
-polyq_status launched() { return hipGetLastError() == hipSuccess ? POLYQ_OK : POLYQ_ERR_DEVICE; }
-
 template <class T>
 polyq_status quantize(const T* x, int32_t rows, int32_t k, uint8_t* packed, uint8_t* xt, hipStream_t st) {
   const int records = records_of(k), tiles = xt ? static_cast<int>(align_up(rows, 64) / kRows) : tiles_of(rows);

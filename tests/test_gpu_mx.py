@@ -219,12 +219,12 @@ def test_gated_tiles(m, n, k):
         assert bool(((h.double() - want).abs() <= tol + out_tol(want, typ)).all()), (typ, m, n, k)
 
 
-# Shapes that reach every tile of the gradients' products: 256 x 256, 256 x 128 (few tokens) and 256 x 64, with and
-# without a split reduction.
-GRADS = [(64, 8192, 4096), (40, 5120, 2000), (300, 4100, 4352), (1100, 2200, 5120), (2000, 1000, 5120), (520, 13824, 640)]
+# Shapes that reach every tile of the gradients' products: 256 x 256, 256 x 64 and 128 x 64 of either product, with and
+# without a split reduction, one and three terms.
+GRADS = [(64, 8192, 4096), (500, 1024, 9000), (70, 3000, 1500), (40, 5120, 2000), (300, 4100, 4352), (1100, 2200, 5120), (2000, 1000, 5120), (520, 13824, 640)]
 
 
-@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("t", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("m,n,k", GRADS)
 def test_linear_backward_tiles(m, n, k, t):
     g = torch.Generator(device=dev()).manual_seed(m)
@@ -233,7 +233,7 @@ def test_linear_backward_tiles(m, n, k, t):
     dy = torch.randn((m, n), generator=g, device=dev()).to(F[t])
     xv, wv, _, _ = device_linear(x, w)
     d = dy.double()
-    terms = {"bf16": 1, "fp32": 3}[t]
+    terms = {"bf16": 1, "fp16": 2, "fp32": 3}[t]
     for got, want, mag, length in zip(pq.mx_linear_backward(dy, x, pq.mx_quantize(w)), (d @ wv, d.T @ xv),
                                       (d.abs() @ wv.abs(), d.abs().T @ xv.abs()), (n, m)):
         tol = 2.0 ** -23 * (terms * (length // 32 + 2) + 40) * mag + out_tol(want, F[t])
