@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "internal.h"
 
 namespace polyq {
@@ -325,9 +327,10 @@ __device__ __forceinline__ void transpose_chunk(uint8_t* lds, i4v codes, uint32_
 // P(-a) = exp(-a^2 / 2) t p(t), t = 1 / (1 + 0.318 a): p, of degree 9, was fitted to
 // exp(z^2) erfc(z) / (2 t) over z = a / sqrt 2 >= 0 (least squares reweighted to an even relative
 // error: 3.3e-8).
-__device__ __forceinline__ float activation(int act, float g, float* slope) {
+template <int ACT>
+__device__ __forceinline__ float activation(float g, float* slope) {
   const float log2e = 1.44269504088896341f;
-  if (act == POLYQ_ACT_GELU) {
+  if constexpr (ACT == POLYQ_ACT_GELU) {
     const float a = __builtin_fabsf(g);
     const float t = __builtin_amdgcn_rcpf(1.f + 0.318198051533946f * a);
     float p = -0.02069910056889057f;
@@ -345,7 +348,7 @@ __device__ __forceinline__ float activation(int act, float g, float* slope) {
     if (slope) *slope = P + g * (0.39894228040143268f * e);
     return g * P;
   }
-  if (act == POLYQ_ACT_GELU_TANH) {
+  if constexpr (ACT == POLYQ_ACT_GELU_TANH) {
     const float a = 0.79788456080286536f, b = 0.044715f, g2 = g * g;
     const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.f * log2e * a * g * (1.f + b * g2)));
     // s (1 - s) is 0 where z' overflows the product
@@ -355,6 +358,12 @@ __device__ __forceinline__ float activation(int act, float g, float* slope) {
   const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-log2e * g));
   if (slope) *slope = s * (1.f + g * (1.f - s));
   return g * s;
+}
+// The same with the activation known at run time.
+__device__ __forceinline__ float activation(int act, float g, float* slope) {
+  if (act == POLYQ_ACT_GELU) return activation<POLYQ_ACT_GELU>(g, slope);
+  if (act == POLYQ_ACT_GELU_TANH) return activation<POLYQ_ACT_GELU_TANH>(g, slope);
+  return activation<POLYQ_ACT_SILU>(g, slope);
 }
 inline bool valid_act(int act) { return act == POLYQ_ACT_SILU || act == POLYQ_ACT_GELU || act == POLYQ_ACT_GELU_TANH; }
 

@@ -202,21 +202,51 @@ def test_linear_tiles(m, n, k):
         assert bool(((y.double() - want).abs() <= tol).all()), (typ, m, n, k)
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("m,n,k", TILES)
-def test_gated_tiles(m, n, k):
+def test_gated_tiles(m, n, k, act):
     g = torch.Generator(device=dev()).manual_seed(m)
     x = torch.randn((m, k), generator=g, device=dev()).bfloat16()
     gate, up = (torch.randn((n, k), generator=g, device=dev()) * 0.05 for _ in range(2))
     _, _, gw, gm = device_linear(x, gate)
     _, _, uw, um = device_linear(x, up)
-    a = act64("silu", gw)[0]
+    a = act64(act, gw)[0]
     ea, eu = 1.2 * sum_tol(gm, k) + act_tol(gw, a), sum_tol(um, k)
     want = a * uw
     tol = (ea * uw.abs() + (a.abs() + ea) * eu + 2.0 ** -23 * want.abs()) * (1 + 2.0 ** -8)
     gq, uq = pq.mx_quantize(gate), pq.mx_quantize(up)
     for typ in (torch.float32, torch.bfloat16):
-        h = pq.mx_gated(x, gq, uq, dtype=typ)
+        h = pq.mx_gated(x, gq, uq, act=act, dtype=typ)
         assert bool(((h.double() - want).abs() <= tol + out_tol(want, typ)).all()), (typ, m, n, k)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("t", ["bf16", "fp32"])
+@pytest.mark.parametrize("m,n,k", [(300, 2050, 384), (1100, 2304, 384), (520, 8192, 260)])
+def test_gated_backward_tiles(m, n, k, t, act):
+    """The backward's own tiles of g and u, whole ones and ragged ones, and two matrices in one sum."""
+    typ = F[t]
+    g = torch.Generator(device=dev()).manual_seed(m)
+    x = torch.randn((m, k), generator=g, device=dev()).to(typ)
+    gate, up = (torch.randn((n, k), generator=g, device=dev()) * 0.05 for _ in range(2))
+    d = torch.randn((m, n), generator=g, device=dev()).to(typ)
+    xv, gv, gw, gm = device_linear(x, gate)
+    _, uv, uw, um = device_linear(x, up)
+    a, da = act64(act, gw)
+    eg, eu = sum_tol(gm, k), sum_tol(um, k)
+    got = pq.mx_gated_backward(d, x, pq.mx_quantize(gate), pq.mx_quantize(up), act=act)
+    d = d.double()
+    dg, du = d * uw * da, d * a
+    curve = 1.2 * eg + act_tol(gw, da) + act_tol(gw, a)
+    e_dg = d.abs() * (curve * (uw.abs() + eu) + eu * da.abs()) + (TERM[typ] + 2.0 ** -22) * dg.abs()
+    e_du = d.abs() * (1.2 * eg + act_tol(gw, a)) + (TERM[typ] + 2.0 ** -22) * du.abs()
+    terms = {"bf16": 1, "fp32": 3}[t]
+    for out, want, mag, err, length in (
+            (got[0], dg @ gv + du @ uv, dg.abs() @ gv.abs() + du.abs() @ uv.abs(), e_dg @ gv.abs() + e_du @ uv.abs(), 2 * n),
+            (got[1], dg.T @ xv, dg.abs().T @ xv.abs(), e_dg.T @ xv.abs(), m),
+            (got[2], du.T @ xv, du.abs().T @ xv.abs(), e_du.T @ xv.abs(), m)):
+        tol = err + 2.0 ** -23 * (terms * (length // 32 + 2) + 40) * (mag + err)
+        assert bool(((out.double() - want).abs() <= tol * (1 + HALF[typ]) + out_tol(want, typ)).all()), (m, n, k, t, act)
 
 
 # Shapes that reach every tile of the gradients' products: 256 x 256, 256 x 64 and 128 x 64 of either product, with and
