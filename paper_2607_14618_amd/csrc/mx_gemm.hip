@@ -329,11 +329,11 @@ __global__ __launch_bounds__(64 * W, 2) void mx_split_kernel(const Args a) {
 // clock; so it is 64 there and 48 of 64 from the caches.  Fragments are read half a chunk ahead
 // of their products, in the order written (the scheduler would sink them to their uses).
 // What bounds it: the matrix cores and what their power leaves.  On random values a loop of nothing but these
-// instructions reaches 6.5 to 7.0 PFLOP/s (clocks fall to 2.0 GHz), gate/up of 2000 tokens x 13824 x 5120 3.7 (153 us, of
-// which 1728 work-groups in rounds of 512 leave a sixth idle, loads cost 20 and the epilogue 30), the down projection
-// 3.4 (82 us).  Measured on the way for the former: 16x16x128 instructions and both operands in LDS 228 us, weights in
+// instructions reaches 6.5 to 7.0 PFLOP/s (clocks fall to 2.0 GHz), gate/up of 2000 tokens x 13824 x 5120 3.9 (146 us:
+// products alone 88, in which 1728 work-groups in rounds of 512 leave a sixth idle, loads of weights 20, of scales 10 and
+// tokens 14, stores 10), the down projection 3.4 (82 us).  Measured on the way for the former: 16x16x128 instructions and both operands in LDS 228 us, weights in
 // registers 205, 32x32x64 instructions and buffer loads into LDS (after the global form the compiler waits for all loads)
-// 176, activations by hardware exp2 and reciprocal 157, 16-byte stores 153.  One wave per SIMD with twice the tile: 247.
+// 176, activations by hardware exp2 and reciprocal 157, 16-byte stores 153, one branch for all activations 146.  One wave per SIMD with twice the tile: 247.
 template <int MODE, int WN, int WM, int TN, int TM, int AHEAD>
 __global__ __launch_bounds__(64 * WN * WM, 2) void mx_gemm_kernel(const Args a) {
   constexpr int W = WN * WM, CT = WM * TM;
