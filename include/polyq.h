@@ -526,7 +526,8 @@ polyq_status polyq_mx_gated(const void* x, int32_t x_type, int32_t m, const void
  * as if it were the identity:
  *   dx = dy W  [m][k],   dw = dy^T q(x)  [n][k],   both of grad_type, either NULL to skip
  *   (not both; x may be NULL where dw is).  dy [m][n] of dy_type.
- * The products run on the bf16 matrix cores, summed in fp32: W and q(x) are exact in
+ * m and n up to 2^21 (else POLYQ_ERR_CAPACITY).  The products run on the bf16 matrix
+ * cores, summed in fp32: W and q(x) are exact in
  * bf16, dy enters as one bf16 value where grad_type is bf16, as the sum of two for
  * fp16 (to 2^-17) and of three for fp32 (exactly).
  *   workspace: polyq_mx_linear_backward_workspace_bytes(m, n, k, x_type, grad_type, dx,

@@ -93,7 +93,7 @@ def mx_quantize(x: torch.Tensor) -> MXMatrix:
     t = _type(x.dtype, "x")
     x2 = _two(x, "x")
     dev = _need_cuda(x2)
-    out = _empty_matrix(x2.shape[0], x2.shape[1], dev)
+    out = _empty_matrix(*x2.shape, dev)
     _launch("polyq_mx_quantize", dev, x2.data_ptr(), t, out.rows, out.k, out.packed.data_ptr())
     return out
 
@@ -134,20 +134,19 @@ def mx_unpack(q: MXMatrix) -> Tuple[torch.Tensor, torch.Tensor]:
 Activations = Union[torch.Tensor, MXMatrix]
 
 
-def _input(x: Activations, *ws: MXMatrix):
-    """(x's pointer, its type, tokens, the default output type) with the weights' shapes checked."""
-    for w in ws:
-        if not isinstance(w, MXMatrix):
-            raise ValueError("weights must be packed (mx_quantize or mx_pack)")
-        if w.shape != ws[0].shape:
-            raise ValueError(f"gate {ws[0].shape} and up {w.shape} must have the same shape")
+def _input(x: Activations, w: MXMatrix, up: Optional[MXMatrix] = None):
+    """(x's tensor, its type, tokens, the default output type) with the weights' shapes checked."""
+    if not isinstance(w, MXMatrix) or not (up is None or isinstance(up, MXMatrix)):
+        raise ValueError("weights must be packed (mx_quantize or mx_pack)")
+    if up is not None and (up.rows != w.rows or up.k != w.k):
+        raise ValueError(f"gate {w.shape} and up {up.shape} must have the same shape")
     if isinstance(x, MXMatrix):
         t, m, k, out, held = PACKED, x.rows, x.k, torch.bfloat16, x.packed
     else:
-        t, held = _type(x.dtype, "x"), _two(x, "x")
-        m, k, out = held.shape[0], held.shape[1], x.dtype
-    if k != ws[0].k:
-        raise ValueError(f"x has {k} channels, the weights have {ws[0].k}")
+        t, held, out = _type(x.dtype, "x"), _two(x, "x"), x.dtype
+        m, k = held.shape
+    if k != w.k:
+        raise ValueError(f"x has {k} channels, the weights have {w.k}")
     return held, t, m, out
 
 
@@ -169,25 +168,24 @@ def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev: torch.device):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
-def _product(x: Activations, ws, act: Optional[int], dtype, y, workspace):
-    held, t, m, out = _input(x, *ws)
-    w = ws[0]
-    dev = _need_cuda(held, y, workspace, *[v.packed for v in ws])
+def _product(x: Activations, w: MXMatrix, up: Optional[MXMatrix], act: int, dtype, y, workspace):
+    held, t, m, out = _input(x, w, up)
+    dev = _need_cuda(held, w.packed, None if up is None else up.packed, y, workspace)
     dtype = y.dtype if dtype is None and y is not None else out if dtype is None else dtype
     ot = _type(dtype, "the output")
     y = _output(y, (m, w.rows), dtype, dev, "the output")
     if t == PACKED:
         need = 0
-    elif act is None:
+    elif up is None:
         need = lib().polyq_mx_linear_workspace_bytes(m, w.k, t)
     else:
         need = lib().polyq_mx_gated_workspace_bytes(m, w.k, t)
     ptr, nbytes, _keep = _scratch(workspace, need, dev)
-    if act is None:
+    if up is None:
         _launch("polyq_mx_linear", dev, held.data_ptr(), t, m, w.packed.data_ptr(), w.rows, w.k, y.data_ptr(), ot, ptr,
                 nbytes)
     else:
-        _launch("polyq_mx_gated", dev, held.data_ptr(), t, m, w.packed.data_ptr(), ws[1].packed.data_ptr(), w.rows, w.k,
+        _launch("polyq_mx_gated", dev, held.data_ptr(), t, m, w.packed.data_ptr(), up.packed.data_ptr(), w.rows, w.k,
                 act, y.data_ptr(), ot, ptr, nbytes)
     return y
 
@@ -197,14 +195,17 @@ def mx_linear(x: Activations, w: MXMatrix, dtype: Optional[torch.dtype] = None, 
     """y [m][n] = q(x) W^T, q(x) the microscaled 4-bit form of x.  x is [m][k] (fp32,
     fp16 or bf16; one row as [k]) or a packed matrix, which several products can share;
     y has x's type (bf16 for a packed x) unless ``dtype`` or ``y`` says otherwise."""
-    return _product(x, (w,), None, dtype, y, workspace)
+    return _product(x, w, None, 0, dtype, y, workspace)
 
 
 def mx_gated(x: Activations, gate: MXMatrix, up: MXMatrix, act: str = "silu", dtype: Optional[torch.dtype] = None,
              y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """h [m][n] = act(q(x) gate^T) * (q(x) up^T) in one launch; act: "silu", "gelu" or
     "gelu_tanh".  x, dtype and y as for ``mx_linear``."""
-    return _product(x, (gate, up), _act(act), dtype, y, workspace)
+    a = _act(act)
+    if up is None:
+        raise ValueError("weights must be packed (mx_quantize or mx_pack)")
+    return _product(x, gate, up, a, dtype, y, workspace)
 
 
 def _act(act: str) -> int:
@@ -258,6 +259,8 @@ def mx_gated_backward(dh: torch.Tensor, x: Activations, gate: MXMatrix, up: MXMa
     a = _act(act)
     if not (need_dx or need_dw):
         raise ValueError("neither dx nor the weights' gradients are asked for")
+    if up is None:
+        raise ValueError("weights must be packed (mx_quantize or mx_pack)")
     held, t, m, _ = _input(x, gate, up)
     n, k = gate.shape
     d, dt = _incoming(dh, m, n, "dh")

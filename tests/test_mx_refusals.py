@@ -80,7 +80,8 @@ BACK_GOOD = dict(d=P, dt=2, x=P, xt=2, m=2, w=P, n=16, k=64, dx=P, dw=P, gt=2, w
 BACK_BAD = [(dict(d=NULL), ARG), (dict(x=NULL), ARG), (dict(w=NULL), ARG), (dict(dt=3), ARG), (dict(xt=5), ARG),
             (dict(gt=3), ARG), (dict(m=0), ARG), (dict(n=0), SHAPE), (dict(k=0), SHAPE), (dict(dx=NULL, dw=NULL), ARG),
             (dict(d=ODD), ARG), (dict(dx=ODD), ARG), (dict(dw=ODD), ARG), (dict(w=ODD), ARG), (dict(x=ODD), ARG),
-            (dict(ws=NULL), CAPACITY), (dict(wsb=100), CAPACITY), (dict(ws=ODD), ARG)]
+            (dict(ws=NULL), CAPACITY), (dict(wsb=100), CAPACITY), (dict(ws=ODD), ARG),
+            (dict(m=(1 << 21) + 1), CAPACITY), (dict(n=(1 << 21) + 1), CAPACITY)]
 
 
 @pytest.mark.parametrize("change,want", BACK_BAD)
@@ -111,6 +112,11 @@ def test_binding_refusals():
         pq.mx_linear(torch.zeros((4, 63)), w)
     with pytest.raises(ValueError, match="packed"):
         pq.mx_linear(cpu, cpu)
+    for bad in (None, cpu):
+        with pytest.raises(ValueError, match="packed"):
+            pq.mx_gated(cpu, w, bad)
+        with pytest.raises(ValueError, match="packed"):
+            pq.mx_gated_backward(torch.zeros((4, 16)), cpu, w, bad)
     with pytest.raises(ValueError, match="GPU tensors"):
         pq.mx_linear(cpu, w)
     with pytest.raises(ValueError, match="act must be"):
