@@ -527,9 +527,10 @@ polyq_status polyq_mx_gated(const void* x, int32_t x_type, int32_t m, const void
  *   dx = dy W  [m][k],   dw = dy^T q(x)  [n][k],   both of grad_type, either NULL to skip
  *   (not both; x may be NULL where dw is).  dy [m][n] of dy_type.
  * m and n up to 2^21 (else POLYQ_ERR_CAPACITY).  The products run on the bf16 matrix
- * cores, summed in fp32: W and q(x) are exact in
- * bf16, dy enters as one bf16 value where grad_type is bf16, as the sum of two for
- * fp16 (to 2^-17) and of three for fp32 (exactly).
+ * cores, summed in fp32: W and q(x) are exact in bf16 (values from 2^128 on, which no
+ * float holds, are infinities), dy enters as one bf16 value where grad_type is bf16 (to
+ * 2^-8; exactly if dy is bf16), as the sum of two for fp16 (to 2^-17) and of three for
+ * fp32 (exactly, but for bits below 2^-133).  A finite dy stays finite.
  *   workspace: polyq_mx_linear_backward_workspace_bytes(m, n, k, x_type, grad_type, dx,
  *   dw) bytes (dx, dw: whether that gradient is asked for), 256-byte aligned.
  */
@@ -543,7 +544,8 @@ polyq_status polyq_mx_linear_backward(const void* dy, int32_t dy_type, const voi
 /*
  * polyq_mx_gated_backward -- gradients of polyq_mx_gated from dh [m][n]; g and u are
  * computed again from x, gate and up:
- *   dg = dh u act'(g),  du = dh act(g)   in fp32, then as dy above,
+ *   dg = dh u act'(g),  du = dh act(g)   in fp32, then as dy above (in bf16 an error of
+ *        its own, as large as that of rounding the result; an fp16 or fp32 grad_type has less),
  *   dx = dg G + du U,  dgate = dg^T q(x),  dup = du^T q(x),
  * of grad_type; dx, or dgate and dup together, may be NULL to skip them.  workspace as
  * above (polyq_mx_gated_backward_workspace_bytes).

@@ -252,14 +252,20 @@ __device__ __forceinline__ void store4(void* base, int type, int64_t at, f4 v, b
   else store4(static_cast<__bf16*>(base) + at, v, vec, valid);
 }
 
-// The next bf16 terms of fp32 values, and what they leave of them (nothing of one that is not finite in bf16).
-__device__ __forceinline__ bf16x4 next_terms(f4* v) {
+// bf16 term `term` of `terms` of fp32 values, and what it leaves of them (nothing of one that is not finite).  A term is the
+// nearest bf16 value; but one that would be an infinity (from 2^128 - 2^119 on) and the second of three are cut towards
+// zero, so that no sum of the first terms lies past the largest float.  One term is within 2^-8 of the value, two are
+// within 2^-17, and three are exactly the value, but for bits below 2^-133, the smallest of bf16.
+__device__ __forceinline__ bf16x4 next_terms(f4* v, int term, int terms) {
+  const bool cut = term > 0 && term + 1 < terms;
   bf16x4 t;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    t[i] = static_cast<__bf16>((*v)[i]);
-    const float f = static_cast<float>(t[i]);
-    (*v)[i] = __builtin_isfinite(f) ? (*v)[i] - f : 0.f;
+    const float x = (*v)[i];
+    t[i] = static_cast<__bf16>(x);
+    if (__builtin_isfinite(x) && (cut || !__builtin_isfinite(static_cast<float>(t[i]))))
+      t[i] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(__builtin_bit_cast(uint32_t, x) >> 16));
+    (*v)[i] = __builtin_isfinite(x) ? x - static_cast<float>(t[i]) : 0.f;
   }
   return t;
 }
@@ -380,8 +386,7 @@ polyq_status launch_quantize(const void* x, int type, int32_t rows, int32_t k, v
                              void* transposed = nullptr);
 
 // dg and du of the gated block as bf16 planes [terms][2][m_pad][n_pad] in blocks (plane_at; zero behind m and
-// n), whose sum over the terms is the fp32 value: to 2^-9, 2^-17 and 2^-25 of it with one,
-// two and three.  x is packed.
+// n), whose sum over the terms is the fp32 value as near as next_terms brings it.  x is packed.
 polyq_status launch_gated_grad(const void* gate, const void* up, const void* x, const void* dh, int dh_type, int32_t m,
                                int32_t n, int32_t k, int act, void* planes, int terms, int32_t m_pad, int32_t n_pad,
                                hipStream_t st);

@@ -78,8 +78,8 @@ __device__ __forceinline__ void finish(const Args& a, int token, int n0, f4 v, f
     const int64_t plane = static_cast<int64_t>(a.m_pad) * a.n_pad * 2;
     uint8_t* out = static_cast<uint8_t*>(a.y) + plane_at(token, n0, a.n_pad);
     for (int t = 0; t < a.terms; ++t) {
-      *reinterpret_cast<bf16x4*>(out + 2 * t * plane) = next_terms(&dg);
-      *reinterpret_cast<bf16x4*>(out + (2 * t + 1) * plane) = next_terms(&du);
+      *reinterpret_cast<bf16x4*>(out + 2 * t * plane) = next_terms(&dg, t, a.terms);
+      *reinterpret_cast<bf16x4*>(out + (2 * t + 1) * plane) = next_terms(&du, t, a.terms);
     }
   } else {
     if (token >= a.m || n0 >= a.n) return;
@@ -100,7 +100,8 @@ __device__ __forceinline__ void finish_pair(const Args& a, int token, int n0, in
     const int64_t plane = static_cast<int64_t>(a.m_pad) * a.n_pad * 2;
     uint8_t* out = static_cast<uint8_t*>(a.y) + plane_at(token, n0 - 4 * upper, a.n_pad) + upper * 16;
     for (int t = 0; t < a.terms; ++t) {
-      const bf16x4 g0 = next_terms(&dg), g1 = next_terms(&dg8), u0 = next_terms(&du), u1 = next_terms(&du8);
+      const bf16x4 g0 = next_terms(&dg, t, a.terms), g1 = next_terms(&dg8, t, a.terms);
+      const bf16x4 u0 = next_terms(&du, t, a.terms), u1 = next_terms(&du8, t, a.terms);
       *reinterpret_cast<u4v*>(out + 2 * t * plane) = pack_halves(g0, g1);
       *reinterpret_cast<u4v*>(out + (2 * t + 1) * plane) = pack_halves(u0, u1);
     }

@@ -6,8 +6,8 @@
 // matrix instructions do not apply: W and x^ are converted to bf16 (exact: two
 // significant bits and a power of two) and multiplied on the bf16 matrix cores.  d
 // comes as planes of bf16 terms whose sum is the value (launch_gated_grad): one term for
-// gradients in bf16 (an error of 2^-9 per factor, as large as the result's own rounding),
-// two for fp16, three for fp32.
+// gradients in bf16 (an error of at most 2^-8 per factor, as large as the result's own rounding),
+// two for fp16 (2^-17), three for fp32 (next_terms says how exact).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -357,7 +357,8 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const void* __restrict__
   f4 v = {0.f, 0.f, 0.f, 0.f};
   if (row < m && col < n) v = load4(d, type, static_cast<int64_t>(row) * n + col, vec, n - col);
   for (int t = 0; t < terms; ++t)
-    *reinterpret_cast<bf16x4*>(planes + t * (static_cast<int64_t>(m_pad) * n_pad * 2) + plane_at(row, col, n_pad)) = next_terms(&v);
+    *reinterpret_cast<bf16x4*>(planes + t * (static_cast<int64_t>(m_pad) * n_pad * 2) + plane_at(row, col, n_pad)) =
+        next_terms(&v, t, terms);
 }
 
 inline int64_t pad64(int64_t v) { return align_up(v, 64); }
