@@ -1,5 +1,5 @@
-// Shared definitions of the microscaled 4-bit (MXFP4) operators: the packed layout
-// (include/polyq.h, polyq_mx_bytes), the operand fragments it is made of, element
+// Shared device code of the microscaled 4-bit (MXFP4) operators: the packed layout's
+// operand fragments (include/polyq.h, polyq_mx_bytes; sizes in mx_plan.h), element
 // types and the gated block's activations.  Not part of the public ABI.
 #pragma once
 
@@ -8,18 +8,11 @@
 
 #include <type_traits>
 
-#include "internal.h"
+#include "mx_plan.h"
 
 namespace polyq {
 namespace mx {
 
-constexpr int kBlock = POLYQ_MX_BLOCK;  // values that share a scale
-constexpr int kRows = 16;               // rows of a packed tile: the rows of one matrix instruction
-constexpr int kChunk = 128;             // values of a row that one matrix instruction takes
-constexpr int kChunkBytes = kRows * kChunk / 2;
-constexpr int kRec = 4 * kChunk;        // values of a row that one 4-byte word of scales covers
-constexpr int kScaleBytes = 256;        // scales of a record: a word per lane, its byte c of chunk c
-constexpr int kRecBytes = kScaleBytes + 4 * kChunkBytes;
 constexpr int kNanScale = 255;
 
 typedef int i4v __attribute__((ext_vector_type(4)));
@@ -31,13 +24,6 @@ typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-__host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
-__host__ __device__ inline int chunks_of(int k) { return div_up(k, kChunk); }
-__host__ __device__ inline int records_of(int k) { return div_up(k, kRec); }
-__host__ __device__ inline int tiles_of(int rows) { return div_up(rows, kRows); }
-__host__ __device__ inline int64_t tile_bytes(int k) {
-  return static_cast<int64_t>(records_of(k)) * kScaleBytes + static_cast<int64_t>(chunks_of(k)) * kChunkBytes;
-}
 // Offset of a chunk's codes and of its record's scales inside a tile.
 __host__ __device__ inline int64_t chunk_offset(int c) {
   return static_cast<int64_t>(c >> 2) * kRecBytes + kScaleBytes + (c & 3) * kChunkBytes;

@@ -5,10 +5,9 @@
 // x^ and the weights are multiplied in their 4 bits: a lane's 16 bytes and scale byte of the packed layout are what it
 // hands to a scaled matrix instruction, so nothing is unpacked.  Three kernels: up to 16 tokens read every weight once and
 // are bound by that (mx_stream_kernel), some tokens by latency (mx_split_kernel), many by the matrix cores
-// (mx_gemm_kernel); choose() says which.
+// (mx_gemm_kernel); choose() in mx_plan.h says which.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "mx.h"
@@ -545,41 +544,6 @@ polyq_status run_gemm(Args a, hipStream_t st) {
   const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM, AHEAD>;
   kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(64 * WN * WM), lds, st>>>(a);
   return launched();
-}
-
-// Which kernel a product of more than 16 tokens takes, by estimates in microseconds.
-//   split, TM = 1 or 2 token tiles of 32: 3 us, and the longest of what its work-groups read at 12 MB/us (L2), of
-//     one's own reading at 45 KB/us and of the weights at 5 MB/us (memory);
-//   gemm, 256 rows (gated 128 of each) x 32 TM tokens, TM = 1 .. 4: 5.5 us, and the longer of its chunks and of the
-//     weights at 4.5 MB/us.  A chunk takes a work-group alone on its compute unit {0.15, 0.20, 0.28, 0.36} us,
-//     several {0.20, 0.31, 0.40, 0.50} each.
-// Measured, split 1 / split 2 / gemm of TM = 1, 2, 3, 4 (us): linear of 77 tokens, 5120 x 5120: 9.9 / 10.1 / 11.3, 12.9,
-// 17.8, 21.0; of 256: 19.8 / 17.9 / 11.5, 13.4, 17.5, 20.6; of 64, 5120 x 13824: 17.6 / 20.7 / -, 33.8; of 1000: 108 / 108
-// / 72, 53.6, 46.8, 58.7; of 2000: - / - / 137, 94.9, 81.1, 89.6; gated of 77, 13824 x 5120: 45 / 34 / -, 23, 28, 33; of
-// 2000: - / - / -, 189, 159, 154.
-struct Choice {
-  bool split;
-  int tm;
-};
-Choice choose(int64_t m, int64_t n, int64_t k, int mats) {
-  static const double alone[4] = {0.15, 0.20, 0.28, 0.36}, shared[4] = {0.20, 0.31, 0.40, 0.50};
-  const double row = static_cast<double>(tile_bytes(static_cast<int>(k))) / kRows, weights = row * n * mats;
-  const int64_t chunks = chunks_of(static_cast<int>(k));
-  Choice best = {true, 1};
-  double least = 0;
-  for (int tm = 1; tm <= 2; ++tm) {
-    const int64_t groups = (n + 31) / 32 * ((m + 32 * tm - 1) / (32 * tm));
-    const double bytes = row * 32 * (mats + tm);
-    const double t = 3 + std::max({groups * bytes / 12e6, std::max(1.0, groups / 256.0) * bytes / 45e3, weights / 5e6});
-    if (tm == 1 || t < least) least = t, best = {true, tm};
-  }
-  if (m <= 32) return {true, 1};
-  for (int tm = 1; tm <= 4; ++tm) {
-    const int64_t groups = (n * mats + 255) / 256 * ((m + 32 * tm - 1) / (32 * tm)), each = (groups + 255) / 256;
-    const double t = 5.5 + std::max(chunks * (each == 1 ? alone[tm - 1] : each * shared[tm - 1]), weights / 4.5e6);
-    if (t <= least) least = t, best = {false, tm};
-  }
-  return best;
 }
 
 template <int MODE>

@@ -37,9 +37,6 @@ namespace {
 // x 128 by four waves, two work-groups a compute unit (290, 290); work-groups that walk several outputs with the next one's
 // loads under way (280, 290); L of dW by loads straight into LDS, for which the compiler waits before every transposing
 // read (282, 316).
-constexpr int kStep = 64;            // r of a stage
-constexpr int kMaxRows = 1 << 21;    // tokens and output channels: a work-group's S is reached with 32-bit offsets
-
 struct GradArgs {
   const uint8_t* d;     // planes [terms][mats][p_tiles][n_tiles] of blocks of 32 tokens x 16 n
   const uint8_t* xt;    // dW: [c_tiles][m_tiles] blocks of 32 c x 16 tokens
@@ -362,32 +359,6 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const void* __restrict__
 }
 
 inline int64_t pad64(int64_t v) { return align_up(v, 64); }
-
-// One gradient product's tile (l x s) and splits: 256 x 256 by eight waves where that makes 128 tiles, or 256 x 64 by four;
-// of dx, whose small tiles take all terms in one stage, 128 x 64 where those are few, which makes the stages
-// shorter and more of them at once.  256 x 64 / 128 x 64, dx with its sums (us): 64 tokens, 1024 x 5120 fp32 26.3 / 17.7, 5120 x
-// 5120 bf16 24.3 / 23.6; 500 tokens, 5120 x 13824 102 / 110.
-// The reduction (`steps` stages of each of `terms`) is split where rounds of whole tiles leave much of the GPU idle; a split
-// costs its partial sums, about as much as 8 stages, and has at least 8.
-struct Shape {
-  int l, s, l_blocks, s_blocks, splits;
-};
-Shape grad_shape(bool dw, int l, int s, int outs, int steps, int terms) {
-  Shape h;
-  const bool big = static_cast<int64_t>(div_up(l, 256)) * div_up(s, 256) * outs >= 128;
-  const bool few = !dw && static_cast<int64_t>(div_up(l, 256)) * div_up(s, 64) <= 64;
-  h.l = few ? 128 : 256, h.s = big ? 256 : 64;
-  h.l_blocks = div_up(l, h.l), h.s_blocks = div_up(s, h.s);
-  const int64_t groups = static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs;
-  const int stages = dw || big ? steps * terms : steps, slots = big ? kCUs : few ? 4 * kCUs : 2 * kCUs;  // slots: work-groups at once
-  h.splits = 1;
-  int64_t best = -1;
-  for (int n = 1; n <= 32 && (n == 1 || stages / n >= 8); ++n) {
-    const int64_t rounds = (groups * n + slots - 1) / slots, cost = rounds * ((stages + n - 1) / n + (n > 1 ? 8 : 0));
-    if (best < 0 || cost < best) best = cost, h.splits = n;
-  }
-  return h;
-}
 
 template <bool DW, int WL, int WS, int TL, int TS, int TERMS>
 polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
