@@ -525,21 +525,17 @@ polyq_status run_raw(const Args& a, hipStream_t st) {
 }
 
 template <int MODE, int TM, int W>
-polyq_status run_split(Args a, hipStream_t st) {
+polyq_status run_split(Args a, int64_t groups, hipStream_t st) {
   a.token_blocks = div_up(MODE == kGatedGrad ? a.m_pad : a.m, TM * 32);
-  const int64_t groups = static_cast<int64_t>(div_up(MODE == kGatedGrad ? a.n_pad : a.n, 32)) * a.token_blocks;
-  if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
   const size_t lds = static_cast<size_t>(W) * (MODE == kLinear ? 1 : 2) * TM * 4096;
   mx_split_kernel<MODE, TM, W><<<dim3(static_cast<uint32_t>(groups)), dim3(64 * W), lds, st>>>(a);
   return launched();
 }
 
 template <int MODE, int WN, int WM, int TN, int TM, int AHEAD>
-polyq_status run_gemm(Args a, hipStream_t st) {
-  const int pt = WN * TN / (MODE == kLinear ? 1 : 2);
+polyq_status run_gemm(Args a, int64_t groups, hipStream_t st) {
+  static_assert(WN * TN * 32 == 256, "product_launch");
   a.token_blocks = div_up(MODE == kGatedGrad ? a.m_pad : a.m, WM * TM * 32);
-  const int64_t groups = static_cast<int64_t>(div_up(MODE == kGatedGrad ? a.n_pad : a.n, pt * 32)) * a.token_blocks;
-  if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
   const size_t lds = 16 * static_cast<size_t>(WM * TM) * kChunkBytes;
   const auto kernel = mx_gemm_kernel<MODE, WN, WM, TN, TM, AHEAD>;
   kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(64 * WN * WM), lds, st>>>(a);
@@ -554,12 +550,14 @@ polyq_status run(const Args& a, hipStream_t st) {
     if (a.x_type == POLYQ_MX_BF16) return run_raw<MODE, __bf16>(a, st);
     if (a.m <= 16) return run_stream<MODE, Packed, true>(a, st);
   }
-  const Choice c = choose(a.m, a.n, a.k, MODE == kLinear ? 1 : 2);
-  if (c.split) return c.tm == 1 ? run_split<MODE, 1, 8>(a, st) : run_split<MODE, 2, MODE == kLinear ? 8 : 4>(a, st);
-  if (c.tm == 1) return run_gemm<MODE, 4, 1, 2, 1, 4>(a, st);
-  if (c.tm == 2) return run_gemm<MODE, 4, 1, 2, 2, 4>(a, st);
-  if (c.tm == 3) return run_gemm<MODE, 4, 1, 2, 3, 2>(a, st);
-  return run_gemm<MODE, 4, 1, 2, 4, 2>(a, st);
+  constexpr int mats = MODE == kLinear ? 1 : 2;
+  const Choice c = choose(a.m, a.n, a.k, mats);
+  const int64_t groups = product_launch(c, MODE == kGatedGrad ? a.m_pad : a.m, MODE == kGatedGrad ? a.n_pad : a.n, mats).groups;
+  if (c.split) return c.tm == 1 ? run_split<MODE, 1, 8>(a, groups, st) : run_split<MODE, 2, mats == 1 ? 8 : 4>(a, groups, st);
+  if (c.tm == 1) return run_gemm<MODE, 4, 1, 2, 1, 4>(a, groups, st);
+  if (c.tm == 2) return run_gemm<MODE, 4, 1, 2, 2, 4>(a, groups, st);
+  if (c.tm == 3) return run_gemm<MODE, 4, 1, 2, 3, 2>(a, groups, st);
+  return run_gemm<MODE, 4, 1, 2, 4, 2>(a, groups, st);
 }
 
 }  // namespace
@@ -599,6 +597,8 @@ polyq_status product(const void* x, int x_type, int32_t m, const void* w0, const
   const size_t need = product_bytes(m, k, x_type, act >= 0);
   if (need > 0 && (ws == nullptr || ws_bytes < need)) return POLYQ_ERR_CAPACITY;
   if (need > 0 && !aligned(ws, 256)) return POLYQ_ERR_ARG;
+  if (need > 0 && !launch_fits(record_groups(m, k, false), 256)) return POLYQ_ERR_CAPACITY;
+  if (m > 16 && !product_fits(m, n, k, act < 0 ? 1 : 2, m, n)) return POLYQ_ERR_CAPACITY;
   Args a{};
   a.w[0] = static_cast<const uint8_t*>(w0), a.w[1] = static_cast<const uint8_t*>(w1);
   a.y = y, a.y_type = y_type, a.act = act;

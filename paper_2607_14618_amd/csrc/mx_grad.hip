@@ -345,17 +345,18 @@ __global__ __launch_bounds__(256) void mx_grad_sum_kernel(const GradArgs g) {
   store4(out ? g.out[1] : g.out[0], g.type, at, v, g.vec, valid);
 }
 
-// d [m][n] into the planes, zero in the padding: four elements a thread.
+// d [m][n] into the planes, zero in the padding: four elements a thread at a time.
 __global__ __launch_bounds__(256) void mx_planes_kernel(const void* __restrict__ d, int type, int m, int n, int vec,
                                                         uint8_t* __restrict__ planes, int terms, int m_pad, int n_pad) {
-  const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (id >= static_cast<int64_t>(m_pad) * n_pad / 4) return;
-  const int row = static_cast<int>(id / (n_pad / 4)), col = static_cast<int>(id % (n_pad / 4)) * 4;
-  f4 v = {0.f, 0.f, 0.f, 0.f};
-  if (row < m && col < n) v = load4(d, type, static_cast<int64_t>(row) * n + col, vec, n - col);
-  for (int t = 0; t < terms; ++t)
-    *reinterpret_cast<bf16x4*>(planes + t * (static_cast<int64_t>(m_pad) * n_pad * 2) + plane_at(row, col, n_pad)) =
-        next_terms(&v, t, terms);
+  const int64_t quads = static_cast<int64_t>(m_pad) * n_pad / 4;
+  for (int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; id < quads; id += static_cast<int64_t>(gridDim.x) * 256) {
+    const int row = static_cast<int>(id / (n_pad / 4)), col = static_cast<int>(id % (n_pad / 4)) * 4;
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (row < m && col < n) v = load4(d, type, static_cast<int64_t>(row) * n + col, vec, n - col);
+    for (int t = 0; t < terms; ++t)
+      *reinterpret_cast<bf16x4*>(planes + t * (static_cast<int64_t>(m_pad) * n_pad * 2) + plane_at(row, col, n_pad)) =
+          next_terms(&v, t, terms);
+  }
 }
 
 inline int64_t pad64(int64_t v) { return align_up(v, 64); }
@@ -365,15 +366,13 @@ polyq_status run_tile(const GradArgs& g, int outs, hipStream_t st) {
   const size_t lds = 2 * static_cast<size_t>(WL * TL * 32) * kStep * 2;
   const auto kernel = mx_grad_kernel<DW, WL, WS, TL, TS, TERMS>;
   const int64_t groups = static_cast<int64_t>(g.l_blocks) * g.s_blocks * outs;
-  if (groups > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
   kernel<<<dim3(static_cast<uint32_t>(groups), g.splits), dim3(64 * WL * WS), lds, st>>>(g);
   return launched();
 }
 
 template <bool DW>
-polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
+polyq_status run_grad(GradArgs g, const Shape& h, void* part, hipStream_t st) {
   const int outs = DW ? g.mats : 1;
-  const Shape h = DW ? grad_shape(true, g.n, g.k, outs, g.rsteps, g.terms) : grad_shape(false, g.k, g.m, 1, g.rsteps * g.mats, g.terms);
   g.splits = h.splits, g.l_blocks = h.l_blocks, g.s_blocks = h.s_blocks;
   g.part = static_cast<float*>(part);
   polyq_status r;
@@ -398,24 +397,29 @@ polyq_status run_grad(GradArgs g, void* part, hipStream_t st) {
 struct GradPlan {
   int terms;
   int32_t m_pad, n_pad;
+  Shape dx, dw;
   size_t x_bytes, plane_bytes, xt_bytes, part_bytes, total;
+  bool fits;  // every launch
 };
 GradPlan grad_plan(int32_t m, int32_t n, int32_t k, int mats, int x_type, int grad_type, bool dx, bool dw) {
   // the packed x is what g and u are computed from; the linear layer's gradients need the transposed one alone
-  GradPlan p;
+  GradPlan p{};
   p.terms = grad_type == POLYQ_MX_BF16 ? 1 : grad_type == POLYQ_MX_F16 ? 2 : 3;
   p.m_pad = static_cast<int32_t>(pad64(m)), p.n_pad = static_cast<int32_t>(pad64(n));
   p.x_bytes = x_type == POLYQ_MX_PACKED || mats == 1 ? 0 : align_up(static_cast<int64_t>(polyq_mx_bytes(m, k)), 256);
   p.plane_bytes = static_cast<size_t>(p.terms) * p.m_pad * mats * p.n_pad * 2;
   p.xt_bytes = dw ? static_cast<size_t>(div_up(k, 32)) * (p.m_pad / 16) * kBlockBytes : 0;
-  p.part_bytes = 0;
+  p.fits = (x_type == POLYQ_MX_PACKED || launch_fits(record_groups(m, k, dw), 256)) &&
+           (mats == 1 || product_fits(m, n, k, mats, p.m_pad, p.n_pad));
   if (dx) {
-    const Shape s = grad_shape(false, k, m, 1, mats * (p.n_pad / kStep), p.terms);
-    if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * m * k * 4);
+    p.dx = grad_shape(false, k, m, 1, mats * (p.n_pad / kStep), p.terms);
+    p.fits = p.fits && shape_fits(p.dx, 1, m, k);
+    if (p.dx.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(p.dx.splits) * m * k * 4);
   }
   if (dw) {
-    const Shape s = grad_shape(true, n, k, mats, p.m_pad / kStep, p.terms);
-    if (s.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(s.splits) * mats * n * k * 4);
+    p.dw = grad_shape(true, n, k, mats, p.m_pad / kStep, p.terms);
+    p.fits = p.fits && shape_fits(p.dw, mats, n, k) && (x_type != POLYQ_MX_PACKED || launch_fits(transpose_groups(p.m_pad, k), 256));
+    if (p.dw.splits > 1) p.part_bytes = std::max(p.part_bytes, static_cast<size_t>(p.dw.splits) * mats * n * k * 4);
   }
   p.total = p.x_bytes + p.plane_bytes + p.xt_bytes + p.part_bytes;
   return p;
@@ -444,8 +448,8 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
   if (need_x && !aligned(q.x, q.x_type == POLYQ_MX_PACKED ? 256 : type_bytes(q.x_type))) return POLYQ_ERR_ARG;
   const int size = type_bytes(q.grad_type);
   if (!aligned(q.dx, size) || !aligned(q.dw[0], size) || !aligned(q.dw[1], size)) return POLYQ_ERR_ARG;
-  GradPlan p = grad_plan(q.m, q.n, q.k, q.mats, need_x ? q.x_type : POLYQ_MX_PACKED, q.grad_type, q.dx != nullptr, dw);
-  if (ws == nullptr || ws_bytes < p.total) return POLYQ_ERR_CAPACITY;
+  const GradPlan p = grad_plan(q.m, q.n, q.k, q.mats, need_x ? q.x_type : POLYQ_MX_PACKED, q.grad_type, q.dx != nullptr, dw);
+  if (!p.fits || ws == nullptr || ws_bytes < p.total) return POLYQ_ERR_CAPACITY;
   if (!aligned(ws, 256)) return POLYQ_ERR_ARG;
   uint8_t* at = static_cast<uint8_t*>(ws);
   const void* x = q.x;
@@ -462,10 +466,9 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
                                              p.m_pad, p.n_pad, st);
     if (s != POLYQ_OK) return s;
   } else {
-    const int64_t blocks = (static_cast<int64_t>(p.m_pad) * p.n_pad / 4 + 255) / 256;
-    if (blocks > 0x7FFFFFFFll) return POLYQ_ERR_CAPACITY;
+    const uint32_t blocks = striding_groups(static_cast<int64_t>(p.m_pad) * p.n_pad / 4, 256);
     const int vec = q.n % 4 == 0 && aligned(q.d, 4 * type_bytes(q.d_type));
-    mx_planes_kernel<<<dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st>>>(
+    mx_planes_kernel<<<dim3(blocks), dim3(256), 0, st>>>(
         q.d, q.d_type, q.m, q.n, vec, static_cast<uint8_t*>(planes), p.terms, p.m_pad, p.n_pad);
     const polyq_status s = launched();
     if (s != POLYQ_OK) return s;
@@ -479,14 +482,14 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
   if (q.dx != nullptr) {
     g.out[0] = q.dx, g.rows = q.m, g.rsteps = p.n_pad / kStep;
     g.vec = q.k % 4 == 0 && aligned(q.dx, 4 * size), g.vec16 = q.k % 16 == 0 && aligned(q.dx, 16);
-    const polyq_status s = run_grad<false>(g, part, st);
+    const polyq_status s = run_grad<false>(g, p.dx, part, st);
     if (s != POLYQ_OK) return s;
   }
   if (dw) {
     if (q.x_type == POLYQ_MX_PACKED) {
       const int m_tiles = p.m_pad / 16, c_tiles = div_up(q.k, 32);
-      const int64_t jobs = static_cast<int64_t>(m_tiles) * chunks_of(q.k), blocks = (jobs + 3) / 4;
-      mx_transpose_kernel<<<dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st>>>(static_cast<const uint8_t*>(x), xt, q.m, q.k,
+      const int64_t jobs = static_cast<int64_t>(m_tiles) * chunks_of(q.k);
+      mx_transpose_kernel<<<dim3(static_cast<uint32_t>(transpose_groups(p.m_pad, q.k))), dim3(256), 0, st>>>(static_cast<const uint8_t*>(x), xt, q.m, q.k,
                                                                                     m_tiles, c_tiles, jobs);
       const polyq_status s = launched();
       if (s != POLYQ_OK) return s;
@@ -494,7 +497,7 @@ polyq_status backward(const Request& q, void* ws, size_t ws_bytes, hipStream_t s
     g.out[0] = q.dw[0], g.out[1] = q.dw[1], g.rows = q.n, g.rsteps = p.m_pad / kStep;
     g.vec = q.k % 4 == 0 && aligned(q.dw[0], 4 * size) && aligned(q.dw[1], 4 * size);
     g.vec16 = q.k % 16 == 0 && aligned(q.dw[0], 16) && aligned(q.dw[1], 16);
-    return run_grad<true>(g, part, st);
+    return run_grad<true>(g, p.dw, part, st);
   }
   return POLYQ_OK;
 }

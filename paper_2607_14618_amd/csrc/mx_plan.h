@@ -27,6 +27,20 @@ __host__ __device__ inline int64_t tile_bytes(int k) {
   return static_cast<int64_t>(records_of(k)) * kScaleBytes + static_cast<int64_t>(chunks_of(k)) * kChunkBytes;
 }
 
+// The work-items of a launch have to stay below 2^32 (in each dimension of its grid).
+constexpr int64_t kMaxItems = (1ll << 32) - 1;
+inline bool launch_fits(int64_t groups, int threads) { return groups <= kMaxItems / threads; }
+// Work-groups of one item per thread, as many as a launch holds: the kernel walks what is left with the grid's stride.
+inline uint32_t striding_groups(int64_t items, int threads) {
+  return static_cast<uint32_t>(std::min((items + threads - 1) / threads, kMaxItems / threads));
+}
+
+// Quantization and back: a work-group of 256 per record of a tile (`padded`: rows to whole 64).
+inline int64_t record_groups(int32_t rows, int32_t k, bool padded) {
+  return (padded ? align_up(rows, 64) / kRows : tiles_of(rows)) * static_cast<int64_t>(records_of(k));
+}
+
+// ------------------------------------------------------------------ products
 // Which kernel a product of more than 16 tokens takes, by estimates in microseconds.
 //   split, TM = 1 or 2 token tiles of 32: 3 us, and the longest of what its work-groups read at 12 MB/us (L2), of
 //     one's own reading at 45 KB/us and of the weights at 5 MB/us (memory);
@@ -62,6 +76,22 @@ inline Choice choose(int64_t m, int64_t n, int64_t k, int mats) {
   return best;
 }
 
+// Its launch over n rows of each weight and m tokens (with the padding that it writes).
+struct Launch {
+  int64_t groups;
+  int threads;
+};
+inline Launch product_launch(Choice c, int64_t m, int64_t n, int mats) {
+  const int64_t token_blocks = (m + 32 * c.tm - 1) / (32 * c.tm);
+  if (c.split) return {(n + 31) / 32 * token_blocks, c.tm == 1 || mats == 1 ? 512 : 256};
+  return {(n * mats + 255) / 256 * token_blocks, 256};
+}
+
+inline bool product_fits(int64_t m, int64_t n, int64_t k, int mats, int64_t m_written, int64_t n_written) {
+  const Launch l = product_launch(choose(m, n, k, mats), m_written, n_written, mats);
+  return launch_fits(l.groups, l.threads);
+}
+
 // ------------------------------------------------------------------ gradients
 constexpr int kStep = 64;          // r of a stage
 constexpr int kMaxRows = 1 << 21;  // tokens and output channels: a work-group's S is reached with 32-bit offsets
@@ -90,6 +120,16 @@ inline Shape grad_shape(bool dw, int l, int s, int outs, int steps, int terms) {
     if (best < 0 || cost < best) best = cost, h.splits = n;
   }
   return h;
+}
+
+// Its launches, the sum over the splits of outputs of `rows` x k among them.
+inline bool shape_fits(const Shape& h, int outs, int64_t rows, int64_t k) {
+  return launch_fits(static_cast<int64_t>(h.l_blocks) * h.s_blocks * outs, h.s == 256 ? 512 : 256) &&
+         (h.splits == 1 || launch_fits((rows * k + 1023) / 1024, 256));
+}
+// Transposing packed activations: a work-group of four waves per four chunks of tiles of m_pad rows.
+inline int64_t transpose_groups(int32_t m_pad, int32_t k) {
+  return (static_cast<int64_t>(m_pad / kRows) * chunks_of(k) + 3) / 4;
 }
 
 }  // namespace mx

@@ -112,12 +112,9 @@ __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_kernel(const uint8_
 // and back: a thread per row and block, neighbouring threads on neighbouring rows, that
 // is on neighbouring 16-byte slices of the packed side.
 template <bool PACK, bool VEC>
-__global__ __launch_bounds__(256) void mx_repack_kernel(const uint8_t* __restrict__ in, const uint8_t* __restrict__ in_scales,
-                                                        uint8_t* __restrict__ out, uint8_t* __restrict__ out_scales,
-                                                        int rows, int k, int64_t jobs) {
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (job >= jobs) return;
-  const int slots = records_of(k) * 16;  // blocks of whole records
+__device__ __forceinline__ void repack(const uint8_t* __restrict__ in, const uint8_t* __restrict__ in_scales,
+                                       uint8_t* __restrict__ out, uint8_t* __restrict__ out_scales, int rows, int k,
+                                       int slots, int64_t job) {
   const int row16 = static_cast<int>(job % kRows), block = static_cast<int>(job / kRows % slots);
   const int tile = static_cast<int>(job / kRows / slots);
   const int chunk = block >> 2, q = block & 3;
@@ -166,15 +163,19 @@ __global__ __launch_bounds__(256) void mx_repack_kernel(const uint8_t* __restric
     out_scales[row * blocks + block] = in[scale_at];
   }
 }
-
-// rows and k as they have to be, the work-groups of a launch over `jobs` within the grid's limit
-polyq_status check_jobs(int64_t groups) { return groups > 0x7FFFFFFFll ? POLYQ_ERR_CAPACITY : POLYQ_OK; }
+template <bool PACK, bool VEC>
+__global__ __launch_bounds__(256) void mx_repack_kernel(const uint8_t* __restrict__ in, const uint8_t* __restrict__ in_scales,
+                                                        uint8_t* __restrict__ out, uint8_t* __restrict__ out_scales,
+                                                        int rows, int k, int64_t jobs) {
+  const int slots = records_of(k) * 16;  // blocks of whole records
+  for (int64_t job = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; job < jobs; job += static_cast<int64_t>(gridDim.x) * 256)
+    repack<PACK, VEC>(in, in_scales, out, out_scales, rows, k, slots, job);
+}
 
 template <class T>
 polyq_status quantize(const T* x, int32_t rows, int32_t k, uint8_t* packed, uint8_t* xt, hipStream_t st) {
   const int records = records_of(k), tiles = xt ? static_cast<int>(align_up(rows, 64) / kRows) : tiles_of(rows);
-  const int64_t groups = static_cast<int64_t>(tiles) * records;
-  if (check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
+  const int64_t groups = record_groups(rows, k, xt != nullptr);  // checked by the caller
   const bool vec = aligned(x, 16) && static_cast<int64_t>(k) * sizeof(T) % 16 == 0;
   const auto kernel = xt ? (vec ? mx_quantize_kernel<T, true, true> : mx_quantize_kernel<T, false, true>)
                          : (vec ? mx_quantize_kernel<T, true, false> : mx_quantize_kernel<T, false, false>);
@@ -206,6 +207,7 @@ extern "C" polyq_status polyq_mx_quantize(const void* x, int32_t type, int32_t r
   if (x == nullptr || packed == nullptr || !mx::float_type(type)) return POLYQ_ERR_ARG;
   if (!mx::valid_shape(rows, k)) return POLYQ_ERR_SHAPE;
   if (!mx::aligned(packed, 256) || !mx::aligned(x, mx::type_bytes(type))) return POLYQ_ERR_ARG;
+  if (!mx::launch_fits(mx::record_groups(rows, k, false), 64 * mx::kWaves)) return POLYQ_ERR_CAPACITY;
   return mx::launch_quantize(x, type, rows, k, packed, static_cast<hipStream_t>(stream));
 }
 
@@ -215,8 +217,8 @@ extern "C" polyq_status polyq_mx_dequantize(const void* packed, int32_t rows, in
   if (!mx::valid_shape(rows, k)) return POLYQ_ERR_SHAPE;
   if (!mx::aligned(packed, 256) || !mx::aligned(out, mx::type_bytes(type))) return POLYQ_ERR_ARG;
   const int records = mx::records_of(k);
-  const int64_t groups = static_cast<int64_t>(mx::tiles_of(rows)) * records;
-  if (mx::check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
+  const int64_t groups = mx::record_groups(rows, k, false);
+  if (!mx::launch_fits(groups, 64 * mx::kWaves)) return POLYQ_ERR_CAPACITY;
   const bool vec = mx::aligned(out, 16) && static_cast<int64_t>(k) * mx::type_bytes(type) % 16 == 0;
   const uint8_t* in = static_cast<const uint8_t*>(packed);
   const dim3 grid(static_cast<uint32_t>(groups)), block(64 * mx::kWaves);
@@ -243,12 +245,10 @@ extern "C" polyq_status polyq_mx_pack(const uint8_t* codes, const uint8_t* scale
   if (!mx::valid_shape(rows, k)) return POLYQ_ERR_SHAPE;
   if (!mx::aligned(packed, 256)) return POLYQ_ERR_ARG;
   const int64_t jobs = static_cast<int64_t>(mx::tiles_of(rows)) * mx::kRows * mx::records_of(k) * 16;
-  const int64_t groups = (jobs + 255) / 256;
-  if (mx::check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
   const bool vec = mx::aligned(codes, 16) && (k + 1) / 2 % 16 == 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const auto kernel = vec ? mx::mx_repack_kernel<true, true> : mx::mx_repack_kernel<true, false>;
-  kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(256), 0, st>>>(codes, scales, static_cast<uint8_t*>(packed), nullptr,
+  kernel<<<dim3(mx::striding_groups(jobs, 256)), dim3(256), 0, st>>>(codes, scales, static_cast<uint8_t*>(packed), nullptr,
                                                                     rows, k, jobs);
   return mx::launched();
 }
@@ -259,12 +259,10 @@ extern "C" polyq_status polyq_mx_unpack(const void* packed, int32_t rows, int32_
   if (!mx::valid_shape(rows, k)) return POLYQ_ERR_SHAPE;
   if (!mx::aligned(packed, 256)) return POLYQ_ERR_ARG;
   const int64_t jobs = static_cast<int64_t>(mx::tiles_of(rows)) * mx::kRows * mx::records_of(k) * 16;
-  const int64_t groups = (jobs + 255) / 256;
-  if (mx::check_jobs(groups) != POLYQ_OK) return POLYQ_ERR_CAPACITY;
   const bool vec = mx::aligned(codes, 16) && (k + 1) / 2 % 16 == 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const auto kernel = vec ? mx::mx_repack_kernel<false, true> : mx::mx_repack_kernel<false, false>;
-  kernel<<<dim3(static_cast<uint32_t>(groups)), dim3(256), 0, st>>>(static_cast<const uint8_t*>(packed), nullptr, codes,
+  kernel<<<dim3(mx::striding_groups(jobs, 256)), dim3(256), 0, st>>>(static_cast<const uint8_t*>(packed), nullptr, codes,
                                                                     scales, rows, k, jobs);
   return mx::launched();
 }
