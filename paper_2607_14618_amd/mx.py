@@ -14,6 +14,7 @@ BLOCK = 32
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 PACKED = 3
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+MAX_ROWS, MAX_K = 1 << 24, 1 << 20  # POLYQ_MAX_N, POLYQ_MAX_K; a larger size could not even be handed over (32 bits)
 
 
 # torch's own lookups of the current stream and device build objects around them (2 us of a call's 7).
@@ -37,6 +38,11 @@ def _launch(name: str, dev: torch.device, *args) -> None:
         _check(status, name)
 
 
+def _packed_bytes(rows: int, k: int) -> int:
+    """Bytes of a packed matrix; 0 if it cannot be packed."""
+    return int(lib().polyq_mx_bytes(rows, k)) if 0 < rows <= MAX_ROWS and 0 < k <= MAX_K else 0
+
+
 class MXMatrix:
     """A packed matrix [rows][k] in microscaled 4-bit floating point (polyq.h), as
     ``mx_quantize`` and ``mx_pack`` make it."""
@@ -44,7 +50,7 @@ class MXMatrix:
     __slots__ = ("rows", "k", "packed")
 
     def __init__(self, rows: int, k: int, packed: torch.Tensor):
-        nbytes = int(lib().polyq_mx_bytes(rows, k))
+        nbytes = _packed_bytes(rows, k)
         if nbytes == 0 or packed.dtype != torch.uint8 or not packed.is_contiguous() or packed.numel() < nbytes:
             raise ValueError(f"a packed matrix of {rows} rows x {k} channels is {nbytes} contiguous bytes (uint8)")
         self.rows, self.k, self.packed = rows, k, packed
@@ -76,11 +82,15 @@ def _type(t: torch.dtype, what: str) -> int:
 def _two(x: torch.Tensor, what: str) -> torch.Tensor:
     if x.dim() not in (1, 2):
         raise ValueError(f"{what} must be [rows][columns] or one row")
-    return x if x.dim() == 2 else x.reshape(1, -1)
+    if x.dim() == 1:
+        return x.reshape(1, -1)
+    if x.shape[0] > MAX_ROWS:
+        raise ValueError(f"{what} has {x.shape[0]} rows, at most {MAX_ROWS} are taken")
+    return x
 
 
 def _empty_matrix(rows: int, k: int, dev: torch.device) -> MXMatrix:
-    nbytes = int(lib().polyq_mx_bytes(rows, k))
+    nbytes = _packed_bytes(rows, k)
     if nbytes == 0:
         raise ValueError(f"a matrix of {rows} rows x {k} channels cannot be packed")
     q = MXMatrix.__new__(MXMatrix)

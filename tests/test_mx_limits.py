@@ -3,6 +3,7 @@ report POLYQ_ERR_DEVICE).  No device pointer is dereferenced."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2607_14618_amd as pq
 
@@ -42,3 +43,22 @@ def test_gradients_of_too_many_tiles(m, n, dx, dw, xt):
 def test_gated_gradients_of_too_many_tokens_and_rows():
     m = 1 << 21     # g and u of 2^21 x 2^21
     assert call("polyq_mx_gated_backward", P, 2, P, 3, m, P, P, m, 32, 0, P, None, None, 2, P, HUGE, None) == CAPACITY
+
+
+@pytest.mark.parametrize("rows,k", [((1 << 32) + 16, 64), (16, (1 << 32) + 64), ((1 << 24) + 1, 64), (16, (1 << 20) + 1)])
+def test_sizes_past_32_bits_are_not_cut_to_them(rows, k):
+    """A size of 2^32 + 16 is not 16: the binding refuses what the library's 32-bit arguments cannot hold."""
+    room = torch.zeros(1280, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="packed matrix"):
+        pq.MXMatrix(rows, k, room)
+
+
+def test_more_rows_than_32_bits_hold_are_not_cut_to_them():
+    w = pq.MXMatrix(16, 64, torch.zeros(1280, dtype=torch.uint8))
+    rows = (1 << 32) + 16
+    x, d = torch.zeros(1).expand(rows, 64), torch.zeros(1).expand(rows, 16)
+    for call_ in (lambda: pq.mx_quantize(x), lambda: pq.mx_linear(x, w), lambda: pq.mx_gated(x, w, w),
+                  lambda: pq.mx_linear_backward(d, x, w), lambda: pq.mx_linear_backward(d, None, w, need_dw=False),
+                  lambda: pq.mx_gated_backward(d, x, w, w)):
+        with pytest.raises(ValueError, match="rows"):
+            call_()
