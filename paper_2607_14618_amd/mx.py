@@ -1,6 +1,7 @@
 """Microscaled 4-bit floating point (MXFP4) on one GPU: quantization, the linear layer,
 the gated feed-forward block and their gradients (marshalling around the C ABI).
-Gradients are computed by the ``_backward`` functions; nothing is recorded for autograd."""
+Gradients are computed by the ``_backward`` functions; nothing is recorded for autograd, and a
+product of an x that asks for it is refused."""
 from __future__ import annotations
 
 from typing import Optional, Tuple, Union
@@ -180,6 +181,9 @@ def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev: torch.device):
 
 def _product(x: Activations, w: MXMatrix, up: Optional[MXMatrix], act: int, dtype, y, workspace):
     held, t, m, out = _input(x, w, up)
+    if held.requires_grad and torch.is_grad_enabled():
+        raise ValueError("x requires a gradient, which is not recorded here: call this in the forward of a "
+                         "torch.autograd.Function (or without gradients) and the _backward function in its backward")
     dev = _need_cuda(held, w.packed, None if up is None else up.packed, y, workspace)
     dtype = y.dtype if dtype is None and y is not None else out if dtype is None else dtype
     ot = _type(dtype, "the output")
@@ -204,7 +208,9 @@ def mx_linear(x: Activations, w: MXMatrix, dtype: Optional[torch.dtype] = None, 
               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [m][n] = q(x) W^T, q(x) the microscaled 4-bit form of x.  x is [m][k] (fp32,
     fp16 or bf16; one row as [k]) or a packed matrix, which several products can share;
-    y has x's type (bf16 for a packed x) unless ``dtype`` or ``y`` says otherwise."""
+    y has x's type (bf16 for a packed x) unless ``dtype`` or ``y`` says otherwise.  An x that
+    requires a gradient is taken where none is recorded (torch.no_grad, the forward of an
+    autograd.Function) and refused elsewhere."""
     return _product(x, w, None, 0, dtype, y, workspace)
 
 

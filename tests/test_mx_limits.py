@@ -62,3 +62,17 @@ def test_more_rows_than_32_bits_hold_are_not_cut_to_them():
                   lambda: pq.mx_gated_backward(d, x, w, w)):
         with pytest.raises(ValueError, match="rows"):
             call_()
+
+
+def test_a_gradient_is_not_lost_without_a_word():
+    """An x that requires a gradient is refused where autograd records; what refuses it elsewhere is that it is on the CPU."""
+    w = pq.MXMatrix(16, 64, torch.zeros(1280, dtype=torch.uint8))
+    x = torch.zeros((4, 64), requires_grad=True)
+    for product in (lambda v: pq.mx_linear(v, w), lambda v: pq.mx_gated(v, w, w)):
+        for v in (x, x * 2):
+            with pytest.raises(ValueError, match="requires a gradient"):
+                product(v)
+        with pytest.raises(ValueError, match="GPU tensors"):
+            product(x.detach())
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU tensors"):
+            product(x)
