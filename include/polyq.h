@@ -511,8 +511,9 @@ polyq_status polyq_mx_linear(const void* x, int32_t x_type, int32_t m, const voi
                              size_t workspace_bytes, void* stream);
 
 /*
- * polyq_mx_gated -- the gated feed-forward block's first half in one launch:
+ * polyq_mx_gated -- the gated feed-forward block's first half:
  *   h = act(g) u,  g = q(x) G^T,  u = q(x) U^T   (g, u and act in fp32, h rounded once)
+ * in one launch for a packed x and for up to 2 tokens; more that are not packed are quantized in one before it.
  * gate and up packed [n][k], h [m][n] of h_type; x and workspace as for polyq_mx_linear
  * (polyq_mx_gated_workspace_bytes).
  */

@@ -117,8 +117,8 @@ __device__ __forceinline__ f4 mfma_mx(i4v a, i4v b, f4 c, int sa, int sb) {
 
 // The same for 32 rows x 64 channels of A and B: two row tiles, two of a chunk's four blocks; lane l has
 // row l % 32 and block l / 32, and of D column l % 32, rows 8 i + 4 (l / 32) + 0 .. 3 in elements 4 i .. .
-// Twice the work an instruction: 8.4 PFLOP/s of nothing but these, against 6.1 of the smaller ones, whose
-// longer encoding the instruction stream cannot deliver in time.
+// Twice the work an instruction: a loop of nothing but these reaches 6.5 to 7.0 PFLOP/s on random values, of the smaller
+// ones 5.2 to 6.0 (on constant ones, which take less power, 8.4 to 9.1 against 6.1 to 6.9).
 template <int SEL_A, int SEL_B>
 __device__ __forceinline__ f16v mfma_mx32(i4v a, i4v b, f16v c, int sa, int sb) {
   const i8v x = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, y = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};

@@ -126,8 +126,8 @@ __device__ __forceinline__ void with_type(const Args& a, F f) {
 // two); or `Packed`.
 // What bounds it: memory.  Gate and up of 13824 x 5120, one token: 75 MB in 13 to 15 us (5.0 to 5.7 TB/s), of 25600 x 5120, 16
 // tokens: 139 MB in 28 us (5.0 TB/s); 5120 x 5120, one token: 5.6 us, of which a launch is 2.  Eight waves share K so that a
-// few hundred work-groups have all weights in flight: with 4 waves 14.1 us in place of 15.3 and 29.3 in place of 28.4, with
-// 16 20.2 and 31.9; two row tiles of each matrix a work-group 16.2 and 33.8.
+// few hundred work-groups have all weights in flight: with 4 waves 14.1 us in place of 15.3 and 29.3 in place of 28.4 (there
+// is one launch shape for both, and it is the one for several tokens), with 16 20.2 and 31.9; two row tiles of each matrix a work-group 16.2 and 33.8.
 struct Packed {};
 template <int MODE, class T, bool VEC, int TN, int W>
 __global__ __launch_bounds__(64 * W) void mx_stream_kernel(const Args a) {

@@ -4,7 +4,7 @@
 //   dW[n][c]  = sum_t d[t][n] x^[t][c]
 // The blocks' scales run along c, so they do not factor out of the sums and the 4-bit
 // matrix instructions do not apply: W and x^ are converted to bf16 (exact: two
-// significant bits and a power of two) and multiplied on the bf16 matrix cores.  d
+// significant bits and a power of two, below 2^128) and multiplied on the bf16 matrix cores.  d
 // comes as planes of bf16 terms whose sum is the value (launch_gated_grad): one term for
 // gradients in bf16 (an error of at most 2^-8 per factor, as large as the result's own rounding),
 // two for fp16 (2^-17), three for fp32 (next_terms says how exact).

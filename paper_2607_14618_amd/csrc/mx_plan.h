@@ -46,7 +46,8 @@ inline int64_t record_groups(int32_t rows, int32_t k, bool padded) {
 //     one's own reading at 45 KB/us and of the weights at 5 MB/us (memory);
 //   gemm, 256 rows (gated 128 of each) x 32 TM tokens, TM = 1 .. 4: 5.5 us, and the longer of its chunks and of the
 //     weights at 4.5 MB/us.  A chunk takes a work-group alone on its compute unit {0.15, 0.20, 0.28, 0.36} us,
-//     several {0.20, 0.31, 0.40, 0.50} each.
+//     several {0.20, 0.31, 0.40, 0.50} each.  The weights' term is the same for every TM; where it decides, the largest
+//     tile is taken, which is not always the fastest (gated of 77 below: 33 and not 23).
 // Measured, split 1 / split 2 / gemm of TM = 1, 2, 3, 4 (us): linear of 77 tokens, 5120 x 5120: 9.9 / 10.1 / 11.3, 12.9,
 // 17.8, 21.0; of 256: 19.8 / 17.9 / 11.5, 13.4, 17.5, 20.6; of 64, 5120 x 13824: 17.6 / 20.7 / -, 33.8; of 1000: 108 / 108
 // / 72, 53.6, 46.8, 58.7; of 2000: - / - / 137, 94.9, 81.1, 89.6; gated of 77, 13824 x 5120: 45 / 34 / -, 23, 28, 33; of

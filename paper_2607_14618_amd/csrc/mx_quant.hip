@@ -110,7 +110,9 @@ __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_kernel(const uint8_
 
 // A checkpoint's matrix (two codes a byte, a scale byte per block) into the packed layout
 // and back: a thread per row and block, neighbouring threads on neighbouring rows, that
-// is on neighbouring 16-byte slices of the packed side.
+// is on neighbouring 16-byte slices of the packed side.  Bound by memory: 13824 x 5120 into the packed layout 14.7 us
+// (75 MB read and written, 5.1 TB/s), back 15.9; rows of a length that is no multiple of 16 bytes, whose bytes move
+// one by one, 5120 x 2977: 14.7 and 21.9 us (16 MB).
 template <bool PACK, bool VEC>
 __device__ __forceinline__ void repack(const uint8_t* __restrict__ in, const uint8_t* __restrict__ in_scales,
                                        uint8_t* __restrict__ out, uint8_t* __restrict__ out_scales, int rows, int k,
