@@ -41,14 +41,16 @@ __device__ __forceinline__ float activate(int act, float g, float* slope) {
   else return activation<ACT>(g, slope);
 }
 
-// dg = dh u act'(g), du = dh act(g) of four rows of the weights and one token.
+// dg = dh u act'(g), du = dh act(g) of four rows of the weights and one token.  Where dh u alone is past the largest
+// float, the slope, which may be next to nothing, comes first.
 template <int ACT>
 __device__ __forceinline__ void gated_grad(int act, f4 d, f4 g, f4 u, f4* dg, f4* du) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float slope;
     const float a = activate<ACT>(act, g[i], &slope);
-    (*dg)[i] = d[i] * u[i] * slope;
+    const float product = d[i] * u[i];
+    (*dg)[i] = __builtin_isfinite(product) ? product * slope : u[i] * slope * d[i];
     (*du)[i] = d[i] * a;
   }
 }

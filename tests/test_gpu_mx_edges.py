@@ -7,7 +7,7 @@ import torch
 
 import paper_2607_14618_amd as pq
 from gpu_util import dev
-from test_gpu_mx import F, GRID, HALF, TERM, activations, out_tol, quantized, sum_tol, weights
+from test_gpu_mx import F, GRID, HALF, TERM, act64, activations, out_tol, quantized, sum_tol, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -196,3 +196,21 @@ def test_gated_gradients_next_to_the_largest_value_are_exact():
     want = torch.zeros((n, k))
     want[:, 0] = torch.tensor(TOP)
     assert torch.equal(dgate.cpu(), want)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_gated_gradients_are_finite_where_dh_u_alone_is_not(act):
+    """dh u = 2^140 lies past the largest float, dh u act'(-64) does not (gelu: 0).  Every sum has two products at most;
+    act and its slope are within 2^-24 (16 + 4 x 120) of themselves (act_tol of test_gpu_mx.py at its largest)."""
+    m, n, k = 4, 4, 32
+    x, gate, up = torch.zeros((m, k)), torch.zeros((n, k)), torch.zeros((n, k))
+    x[:, 0], gate[:, 0], up[:, 0] = 1.0, -64.0, 2.0 ** 40
+    dh = torch.eye(m) * 2.0 ** 100
+    got = pq.mx_gated_backward(dh.to(dev()), x.to(dev()), pq.mx_quantize(gate.to(dev())), pq.mx_quantize(up.to(dev())), act=act)
+    a, da = act64(act, torch.full((m, n), -64.0, dtype=torch.float64))
+    dg, du = dh.double() * 2.0 ** 40 * da, dh.double() * a
+    for out, parts in ((got[0], (dg @ gate.double(), du @ up.double())), (got[1], (dg.T @ x.double(),)), (got[2], (du.T @ x.double(),))):
+        want, mag = sum(parts), sum(p.abs() for p in parts)
+        off = (out.cpu().double() - want).abs()
+        assert bool(torch.isfinite(out).all())
+        assert bool((off <= (2.0 ** -24 * (16 + 4 * 120) + 2.0 ** -20) * mag + 1e-30).all()), (act, float(off.max()), float(mag.max()))
